@@ -1,0 +1,14 @@
+// Launchers of the 8-bit layers (not installed).  Arguments have been checked.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "crisp_fp8.h"
+
+namespace crisp {
+
+hipError_t launch_fp8_quant(const void* X, int in_type, int64_t rows, int64_t cols, int64_t ldx, const uint32_t* mask,
+                            const crisp_fp8_mat* Q, const crisp_fp8_mat* Qt, hipStream_t st);
+hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
+                              const crisp_epilogue* ep, hipStream_t st);
+
+}  // namespace crisp

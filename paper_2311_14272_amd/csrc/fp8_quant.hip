@@ -1,0 +1,190 @@
+// Quantisation to e4m3 with one scale for each block of 128 columns of a row, or of 128 x 128 elements: read once, largest
+// magnitude per block, multiply by the scale's inverse, round, write one or both directions.  Bound by memory.
+#include "fp8_common.h"
+#include "fp8_internal.h"
+
+namespace crisp {
+
+// Eight elements of a row from column c on; what lies at or behind `cols` counts as zero.  vec: the address is a multiple of
+// 16 bytes wherever c is a multiple of 8.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* X, int64_t at, int64_t left, bool vec, float (&x)[8]) {
+    if (vec && left >= 8) {
+        if constexpr (BF16) {
+            from_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + at), x);
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
+            const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        x[j] = 0.0f;
+        if (j < left) {
+            if constexpr (BF16) x[j] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(X)[at + j] << 16);
+            else x[j] = static_cast<const float*>(X)[at + j];
+        }
+    }
+}
+
+// ROWS, one direction, no mask: 16 lanes take a block of 128 columns, a workgroup 16 consecutive blocks of the matrix in
+// row order.
+template <bool BF16>
+__global__ __launch_bounds__(256) void fp8_rows_kernel(const void* __restrict__ X, int64_t rows, int cols, int64_t ldx, bool vec,
+                                                       uint8_t* __restrict__ q, int64_t ld, float* __restrict__ scale, int64_t lds) {
+    const int kb = (cols + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int64_t id = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int64_t r = id / kb;
+    const int b = (int)(id - r * kb), lane = threadIdx.x % 16;
+    if (r >= rows) return;      // all 16 lanes of a group leave together
+    const int c = b * FP8_BLOCK + lane * 8;
+    float x[8];
+    load8<BF16>(X, r * ldx + c, cols - c, vec, x);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = umax(top, abs_bits(x[j]));
+    const float s = fp8_scale(__uint_as_float(max16(top))), inv = 1.0f / s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= inv;
+    *reinterpret_cast<uint2*>(q + r * ld + c) = to_fp8x8(x);
+    if (lane == 0) scale[b * lds + r] = s;
+}
+
+// A 128 x 128 tile per workgroup, for everything else.  Thread (g, l): rows 8g .. 8g+7, columns 8l .. 8l+7, held in
+// registers; the transpose is eight bytes per column and thread, gathered in LDS so that it leaves in whole rows.
+template <bool BF16>
+__global__ __launch_bounds__(256) void fp8_tile_kernel(const void* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx, bool vec,
+                                                       const uint32_t* __restrict__ mask, int kind, int tiles_c,
+                                                       uint8_t* __restrict__ q, int64_t ld, float* __restrict__ scale, int64_t lds,
+                                                       uint8_t* __restrict__ qt, int64_t ldt, float* __restrict__ scale_t,
+                                                       int64_t ldst) {
+    __shared__ uint32_t part[4][FP8_BLOCK];          // largest of a column over a wave's rows
+    __shared__ float col_inv[FP8_BLOCK];
+    constexpr int PITCH = FP8_BLOCK + 8;
+    __shared__ __align__(16) uint8_t turned[FP8_BLOCK * PITCH];
+    const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
+    const int tid = threadIdx.x, l = tid % 16, g = tid / 16, wave = tid / 64;
+    const int64_t c = tc * FP8_BLOCK + l * 8, r0 = tr * FP8_BLOCK + g * 8;
+    float x[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t r = r0 + i;
+        load8<BF16>(X, r * ldx + c, r < rows ? cols - c : 0, vec, x[i]);
+    }
+    if (mask) {
+        const int64_t words = (cols + 31) / 32;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = r0 + i < rows && c < cols ? mask[(r0 + i) * words + c / 32] >> (c % 32) : 0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[i][j] = (bits >> j) & 1u ? x[i][j] : 0.0f;
+        }
+    }
+    uint32_t row_top[8], col_top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) col_top[j] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t t = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t a = abs_bits(x[i][j]);
+            t = umax(t, a);
+            col_top[j] = umax(col_top[j], a);
+        }
+        row_top[i] = max16(t);
+    }
+    const bool tiles = kind == CRISP_FP8_TILES;
+    float inv_row[8], inv_col[8];
+    if (tiles || qt) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            col_top[j] = umax(col_top[j], (uint32_t)__shfl_xor((int)col_top[j], 16));
+            col_top[j] = umax(col_top[j], (uint32_t)__shfl_xor((int)col_top[j], 32));
+            if ((tid & 63) < 16) part[wave][l * 8 + j] = col_top[j];
+        }
+        __syncthreads();
+        if (tid < FP8_BLOCK) {
+            uint32_t t = umax(umax(part[0][tid], part[1][tid]), umax(part[2][tid], part[3][tid]));
+            part[0][tid] = t;
+            if (!tiles) {
+                const float s = fp8_scale(__uint_as_float(t));
+                col_inv[tid] = 1.0f / s;
+                if (tc * FP8_BLOCK + tid < cols) scale_t[tr * ldst + tc * FP8_BLOCK + tid] = s;
+            }
+        }
+        __syncthreads();
+        if (tiles) {
+            uint32_t t = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t = umax(t, part[0][l * 8 + j]);
+            const float s = fp8_scale(__uint_as_float(max16(t))), inv = 1.0f / s;
+            if (tid == 0) {
+                if (q) scale[tr * lds + tc] = s;
+                if (qt) scale_t[tc * ldst + tr] = s;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) inv_row[j] = inv_col[j] = inv;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) inv_col[j] = col_inv[l * 8 + j];
+        }
+    }
+    if (q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = r0 + i;
+            if (!tiles) {
+                const float s = fp8_scale(__uint_as_float(row_top[i]));
+                inv_row[i] = 1.0f / s;
+                if (l == 0 && r < rows) scale[tc * lds + r] = s;
+            }
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = x[i][j] * inv_row[i];
+            if (r < rows) *reinterpret_cast<uint2*>(q + r * ld + c) = to_fp8x8(y);
+        }
+    }
+    if (!qt) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i][j] * inv_col[j];
+        *reinterpret_cast<uint2*>(turned + (l * 8 + j) * PITCH + g * 8) = to_fp8x8(y);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int row = tid / 8 + 32 * k;
+        const uint8_t* from = turned + row * PITCH + tid % 8 * 16;
+        const uint2 a = *reinterpret_cast<const uint2*>(from), b = *reinterpret_cast<const uint2*>(from + 8);
+        if (tc * FP8_BLOCK + row < cols)
+            *reinterpret_cast<uint4*>(qt + (tc * FP8_BLOCK + row) * ldt + tr * FP8_BLOCK + tid % 8 * 16) = make_uint4(a.x, a.y, b.x, b.y);
+    }
+}
+
+hipError_t launch_fp8_quant(const void* X, int in_type, int64_t rows, int64_t cols, int64_t ldx, const uint32_t* mask,
+                            const crisp_fp8_mat* Q, const crisp_fp8_mat* Qt, hipStream_t st) {
+    const bool bf16 = in_type == CRISP_IN_BF16;
+    const bool vec = ((uintptr_t)X & 15) == 0 && (ldx * (bf16 ? 2 : 4)) % 16 == 0;
+    const int64_t rb = (rows + FP8_BLOCK - 1) / FP8_BLOCK, cb = (cols + FP8_BLOCK - 1) / FP8_BLOCK;
+    const int kind = Q ? Q->kind : Qt->kind;
+    if (kind == CRISP_FP8_ROWS && !Qt && !mask) {
+        const unsigned grid = (unsigned)((rows * cb + 15) / 16);
+        if (bf16) fp8_rows_kernel<true><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, vec, Q->q, Q->ld, Q->scale, Q->lds);
+        else fp8_rows_kernel<false><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, vec, Q->q, Q->ld, Q->scale, Q->lds);
+        return hipGetLastError();
+    }
+    const crisp_fp8_mat none = {};
+    const crisp_fp8_mat &a = Q ? *Q : none, &b = Qt ? *Qt : none;
+    const unsigned grid = (unsigned)(rb * cb);
+    auto kernel = bf16 ? fp8_tile_kernel<true> : fp8_tile_kernel<false>;
+    kernel<<<grid, 256, 0, st>>>(X, rows, cols, ldx, vec, mask, kind, (int)cb, a.q, a.ld, a.scale, a.lds, b.q, b.ld, b.scale, b.lds);
+    return hipGetLastError();
+}
+
+}  // namespace crisp

@@ -1,0 +1,187 @@
+"""Layers in 8 bits: binding of crisp_fp8_* (include/crisp_fp8.h).  Argument marshalling only, every step runs in the HIP
+kernels.
+
+A matrix in 8 bits (Fp8Mat) is e4m3 values with one fp32 scale for each block of 128 columns of a row (ROWS, activations and
+gradients) or of 128 x 128 elements (TILES, weights).  One layer's training step is
+
+    x8, x_t = quantize_both(x)                   # x: T x K
+    w8, w_t = quantize_both(W, TILES, mask=...)  # W: S x K, after each change of W; mask: pruned positions count as zero
+    y = product(x8, w8)                          # T x S
+    dx, dw = linear_backward(dy, x_t, w_t)       # T x K and S x K, dw in fp32: the gradient crisp_select_mask and adamw take
+
+and serving is y = linear(x, w8).  Tensors live on the current device; work goes to the current stream.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import crisp
+
+ROWS, TILES = 0, 1
+BLOCK = 128
+_IN = {torch.float32: 0, torch.bfloat16: 1}     # CRISP_IN_*, and the CRISP_Y_* of the same types
+
+
+class _Mat(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int64), ("lds", C.c_int64), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("kind", C.c_int32), ("reserved", C.c_int32)]
+
+
+_lib = None
+
+
+def lib():
+    global _lib
+    if _lib is None:
+        L = crisp.lib()
+        vp, i32, i64, mat = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(_Mat)
+        L.crisp_fp8_quant.argtypes = [vp, i32, i64, i64, i64, vp, mat, mat, vp]
+        L.crisp_fp8_product.argtypes = [mat, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp]
+        L.crisp_fp8_linear.argtypes = [vp, i32, i64, i64, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp, C.c_size_t, vp]
+        L.crisp_fp8_linear_ws.argtypes = [i64, i64]
+        for f in (L.crisp_fp8_quant, L.crisp_fp8_product, L.crisp_fp8_linear):
+            f.restype = i32
+        L.crisp_fp8_linear_ws.restype = C.c_size_t
+        _lib = L
+    return _lib
+
+
+def _here(t, what):
+    """A tensor's address; it has to be on the device whose stream the work goes to."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, not on the current GPU" % (what, t.device))
+    return t.data_ptr()
+
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+class Fp8Mat:
+    """A rows x cols matrix in 8 bits over existing tensors: q, rows x at least round_up(cols, 128) bytes (uint8 or
+    float8_e4m3fn, zeros behind the columns), and scale, fp32, ceil(cols/128) x rows (ROWS) or ceil(rows/128) x ceil(cols/128)
+    (TILES); both with contiguous rows, any row stride that the header allows.  Keeps the tensors alive."""
+    __slots__ = ("q", "scale", "rows", "cols", "kind", "c")
+
+    def __init__(self, q, scale, rows, cols, kind):
+        if kind not in (ROWS, TILES):
+            raise ValueError("kind is ROWS or TILES")
+        want = (_blocks(cols), rows) if kind == ROWS else (_blocks(rows), _blocks(cols))
+        if q.dim() != 2 or q.element_size() != 1 or q.shape[0] != rows or q.shape[1] < _blocks(cols) * BLOCK or q.stride(1) != 1:
+            raise ValueError("q: %d rows of at least %d bytes, each row contiguous" % (rows, _blocks(cols) * BLOCK))
+        if scale.dtype != torch.float32 or scale.dim() != 2 or tuple(scale.shape) != want or (scale.stride(1) != 1 and want[1] > 1):
+            raise ValueError("scale: %d x %d fp32, each row contiguous" % want)
+        self.q, self.scale, self.rows, self.cols, self.kind = q, scale, rows, cols, kind
+        # (a tensor of one row may carry any row stride)
+        self.c = _Mat(_here(q, "q"), _here(scale, "scale"), q.stride(0) if rows > 1 else max(q.stride(0), q.shape[1]),
+                      scale.stride(0) if want[0] > 1 else max(scale.stride(0), want[1]), rows, cols, kind, 0)
+
+
+def alloc_mat(rows, cols, kind=ROWS, device="cuda") -> Fp8Mat:
+    """Buffers of a rows x cols matrix in 8 bits, to be filled by quantize."""
+    q = torch.empty((rows, _blocks(cols) * BLOCK), dtype=torch.float8_e4m3fn, device=device)
+    shape = (_blocks(cols), rows) if kind == ROWS else (_blocks(rows), _blocks(cols))
+    return Fp8Mat(q, torch.empty(shape, dtype=torch.float32, device=device), rows, cols, kind)
+
+
+def _input(x):
+    """(address, type, rows, cols, row stride) of a matrix with contiguous rows."""
+    if x.dim() != 2 or x.dtype not in _IN or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("a matrix of fp32 or bf16 with contiguous rows is wanted")
+    rows, cols = x.shape
+    return _here(x, "input"), _IN[x.dtype], rows, cols, x.stride(0) if rows > 1 else max(x.stride(0), cols)
+
+
+def _quant(x, mask, out, out_t):
+    p, kind, rows, cols, ldx = _input(x)
+    if mask is not None and (mask.dtype != torch.int32 or not mask.is_contiguous() or mask.numel() < rows * (-(-cols // 32))):
+        raise ValueError("mask: rows x ceil(cols/32) contiguous int32 words")
+    st = lib().crisp_fp8_quant(p, kind, rows, cols, ldx, None if mask is None else _here(mask, "mask"),
+                               C.byref(out.c) if out is not None else None, C.byref(out_t.c) if out_t is not None else None,
+                               crisp._stream())
+    if st != crisp.OK:
+        raise crisp.CrispError("crisp_fp8_quant", st)
+
+
+def quantize(x, kind=ROWS, mask=None, out=None) -> Fp8Mat:
+    """crisp_fp8_quant of x (fp32 or bf16) into out, allocated when not given.  mask: words as crisp.DeviceLayer.nm_mask or
+    adamw.hybrid_mask hold them; positions whose bit is not set count as zero."""
+    out = alloc_mat(x.shape[0], x.shape[1], kind, x.device) if out is None else out
+    _quant(x, mask, out, None)
+    return out
+
+
+def quantize_both(x, kind=ROWS, mask=None, out=None, out_t=None):
+    """(x, its transpose) in 8 bits, in one pass over x."""
+    out = alloc_mat(x.shape[0], x.shape[1], kind, x.device) if out is None else out
+    out_t = alloc_mat(x.shape[1], x.shape[0], kind, x.device) if out_t is None else out_t
+    _quant(x, mask, out, out_t)
+    return out, out_t
+
+
+def _output(T, S, out, out_dtype, device):
+    if out is None:
+        return torch.empty((T, S), dtype=out_dtype, device=device)
+    if out.dtype not in _IN or tuple(out.shape) != (T, S) or (S > 1 and out.stride(1) != 1):
+        raise ValueError("out: %d x %d of fp32 or bf16 with contiguous rows" % (T, S))
+    return out
+
+
+def _epilogue(ep, bias, S):
+    if bias is None:
+        return ep
+    if ep is not None:
+        raise ValueError("bias goes into the epilogue when there is one")
+    if bias.dtype != torch.float32 or bias.dim() != 1 or bias.numel() != S or (S > 1 and bias.stride(0) != 1):
+        raise ValueError("bias: %d contiguous fp32 values" % S)
+    return crisp.Epilogue(None, _here(bias, "bias"), None, 0, 0, 0)
+
+
+def _ld(y):
+    return y.stride(0) if y.shape[0] > 1 else max(y.stride(0), y.shape[1])
+
+
+def product(x: Fp8Mat, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None):
+    """crisp_fp8_product: x w^T, x.rows x w.rows; into out, allocated as out_dtype when not given.  ep: crisp.epilogue(...),
+    per column of the result."""
+    out = _output(x.rows, w.rows, out, out_dtype, x.q.device)
+    ep = _epilogue(ep, bias, w.rows)
+    st = lib().crisp_fp8_product(C.byref(x.c), C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
+                                 C.byref(ep) if ep is not None else None, crisp._stream())
+    if st != crisp.OK:
+        raise crisp.CrispError("crisp_fp8_product", st)
+    return out
+
+
+def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None, ws=None):
+    """crisp_fp8_linear: the layer for activations x (T x K, fp32 or bf16).  ws: a workspace of the caller's (uint8,
+    crisp_fp8_linear_ws bytes); allocated for the call when not given."""
+    p, kind, T, K, ldx = _input(x)
+    if K != w.cols:
+        raise ValueError("x has %d columns, the weights %d" % (K, w.cols))
+    out = _output(T, w.rows, out, out_dtype, x.device)
+    ep = _epilogue(ep, bias, w.rows)
+    if ws is None:
+        ws = torch.empty(max(16, lib().crisp_fp8_linear_ws(T, K)), dtype=torch.uint8, device=x.device)
+    st = lib().crisp_fp8_linear(p, kind, T, ldx, C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
+                                C.byref(ep) if ep is not None else None, _here(ws, "ws"), ws.numel() * ws.element_size(),
+                                crisp._stream())
+    if st != crisp.OK:
+        raise crisp.CrispError("crisp_fp8_linear", st)
+    return out
+
+
+def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=False):
+    """Gradients of y = linear(x, w): (dx, dw) from dy (T x S, fp32 or bf16), x_t = x^T in 8 bits (K x T) and w_t = W^T in 8
+    bits (K x S).  dx is T x K, bf16 unless given; dw is S x K, fp32 unless given.  accumulate: dw (given) += the gradient."""
+    T, S = dy.shape
+    if x_t.cols != T or w_t.cols != S or x_t.rows != w_t.rows:
+        raise ValueError("dy is %d x %d, x^T %d x %d, W^T %d x %d" % (T, S, x_t.rows, x_t.cols, w_t.rows, w_t.cols))
+    if accumulate and dw is None:
+        raise ValueError("accumulate adds to a dw that is given")
+    dy8, dy_t = quantize_both(dy)
+    dx = product(dy8, w_t, dx)
+    ep = crisp.epilogue(residual=dw, ldr=_ld(dw)) if accumulate else None
+    return dx, product(dy_t, x_t, dw, torch.float32, ep=ep)

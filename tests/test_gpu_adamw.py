@@ -1,0 +1,233 @@
+"""The optimiser step on the GPU against the fp32 form of lowbit_util, which tests/test_lowbit_cpu.py holds to 64 bits: every
+operation is rounded once on both sides, so weights, moments, codes and scales are compared bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2311_14272_amd import adamw, crisp, synth
+
+import lowbit_util as U
+import oracle
+from gpu_util import desc_of, dev
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=0.5, step=5)
+
+
+def _same(a, b):
+    return np.array_equal(np.asarray(a, dtype=np.float64), np.asarray(b, dtype=np.float64), equal_nan=True)
+
+
+def _vals(t):
+    return t.detach().float().cpu().numpy().reshape(-1)
+
+
+class Case:
+    """One tensor with its buffers, and the plain step's results."""
+
+    def __init__(self, rng, n, w32, g32, bits, copy=False, row=0, density=0.5, decay=0.1, wild=True):
+        f = lambda a: torch.from_numpy(np.asarray(a, dtype=np.float32)).cuda()
+        wt, gt = (torch.float32 if b else torch.bfloat16 for b in (w32, g32))
+        self.n, self.w32, self.bits, self.decay, self.row = n, w32, bits, decay, row
+        self.w = f(rng.normal(size=n)).to(wt)
+        size = 10.0 ** rng.uniform(-6, 1, n) if wild else np.ones(n)
+        self.g = f(rng.normal(size=n) * size).to(gt)
+        if bits == 32:
+            self.mom = {"m": f(rng.normal(size=n) * size), "v": f((rng.normal(size=n) * size) ** 2)}
+        else:
+            nb = -(-n // 128)
+            code = lambda a: f(a).to(torch.float8_e4m3fn)
+            self.mom = {"m": code(rng.uniform(-448, 448, n)), "v": code(rng.uniform(0, 448, n) * (rng.random(n) < 0.9)),
+                        "m_scale": f(10.0 ** rng.uniform(-6, 0, nb)), "v_scale": f(10.0 ** rng.uniform(-6, 0, nb))}
+        self.keep = self.mask = None
+        if row:
+            k = rng.random((n // row, row)) < density
+            k[: k.shape[0] // 4] = False                   # rows that keep nothing
+            self.mask = torch.from_numpy(U.bits_of(k)).cuda()
+            self.keep = k.reshape(-1)
+        self.copy = self.w.to(torch.bfloat16) if copy else None
+
+    def tensor(self):
+        return adamw.tensor(self.w, self.g, w_copy=self.copy, mask=self.mask, row_len=self.row, weight_decay=self.decay, **self.mom)
+
+    def plain(self, h):
+        scales = [_vals(self.mom[k]) for k in ("m_scale", "v_scale")] if self.bits == 8 else None
+        return U.adamw(_vals(self.w), _vals(self.g), _vals(self.mom["m"]), _vals(self.mom["v"]), self.keep, h["lr"], h["beta1"],
+                       h["beta2"], h["eps"], h["grad_scale"], h["step"], self.decay, scales, not self.w32)
+
+    def check(self, want):
+        w, m, v, scales = want
+        assert _same(_vals(self.w), w)
+        assert _same(_vals(self.mom["m"]), m) and _same(_vals(self.mom["v"]), v)
+        if scales is not None:
+            assert _same(_vals(self.mom["m_scale"]), scales[0]) and _same(_vals(self.mom["v_scale"]), scales[1])
+        if self.copy is not None:
+            assert _same(_vals(self.copy), U.bf16(w))
+
+
+TYPES = [(w32, g32, bits) for w32 in (True, False) for g32 in (True, False) for bits in (32, 8)]
+
+
+@pytest.mark.parametrize("types", TYPES, ids=lambda t: "w%d-g%d-s%d" % (32 if t[0] else 16, 32 if t[1] else 16, t[2]))
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 9, 127, 128, 129, 255, 1000, 8191, 8192, 8193, 20011])
+def test_one_tensor(n, types):
+    print("adamw", n, types, flush=True)
+    c = Case(np.random.default_rng(n), n, *types, copy=types[0] and n % 2 == 1)
+    want = c.plain(HYPER)
+    adamw.step(adamw.make_batch([c.tensor()]), **HYPER)
+    c.check(want)
+
+
+@pytest.mark.parametrize("types", TYPES, ids=lambda t: "w%d-g%d-s%d" % (32 if t[0] else 16, 32 if t[1] else 16, t[2]))
+@pytest.mark.parametrize("shape", [(1, 1), (3, 5), (7, 8), (5, 31), (40, 33), (64, 64), (9, 1000), (130, 257), (2, 8200)], ids=str)
+def test_masked(shape, types):
+    """Pruned positions keep their weight, lose their moments, and a NaN in their gradient or moments is not seen."""
+    rows, row = shape
+    print("adamw masked", shape, types, flush=True)
+    c = Case(np.random.default_rng(rows * row), rows * row, *types, copy=types[0], row=row)
+    gone = torch.from_numpy(~c.keep).cuda()
+    c.g[gone] = float("nan")
+    before = c.w.clone()
+    want = c.plain(HYPER)
+    if c.bits == 32:
+        c.mom["m"][gone] = float("nan")
+        c.mom["v"][gone] = float("inf")
+    adamw.step(adamw.make_batch([c.tensor()]), **HYPER)
+    c.check(want)
+    assert torch.equal(c.w[gone], before[gone])
+
+
+def test_many_tensors_of_all_types():
+    """More tensors than a launch takes, of all types and sizes mixed, empty ones among them; one that comes twice in a
+    different place would overlap, so each has its own buffers, cut from one so that what lies between them is seen to stay."""
+    rng = np.random.default_rng(4)
+    cases = []
+    for k in range(150):
+        n = int(rng.choice([1, 5, 64, 500, 8192, 9000]))
+        row = n // 5 if n % 5 == 0 and k % 3 == 0 else 0
+        w32, g32, bits = TYPES[k % 8]
+        cases.append(Case(rng, n, w32, g32, bits, copy=w32 and k % 2 == 0, row=row, decay=0.0 if k % 4 else 0.05))
+    want = [c.plain(HYPER) for c in cases]
+    tensors = [c.tensor() for c in cases]
+    empty = torch.empty(0, device="cuda")
+    tensors.insert(3, adamw.tensor(empty, empty, empty, empty))
+    adamw.step(adamw.make_batch(tensors), **HYPER)
+    for c, w in zip(cases, want):
+        c.check(w)
+    adamw.step(adamw.make_batch([adamw.tensor(empty, empty, empty, empty)]), **HYPER)      # nothing to do at all
+
+
+def test_neighbours_stay():
+    """Elements before and behind a tensor's own, in every buffer."""
+    n, at = 1003, 16
+    for types in TYPES:
+        c = Case(np.random.default_rng(1), n, *types, copy=types[0])
+        want = c.plain(HYPER)
+        big = {}
+        for k, t in [("w", c.w), ("g", c.g), ("copy", c.copy)] + list(c.mom.items()):
+            if t is None:
+                continue
+            raw = t.view(torch.uint8) if t.element_size() == 1 else t
+            store = torch.full((t.numel() + 2 * at,), 77, dtype=raw.dtype, device="cuda")
+            store[at:at + t.numel()] = raw
+            big[k] = (store, store[at:at + t.numel()].view(t.dtype))
+        c.w, c.g = big["w"][1], big["g"][1]
+        c.copy = big["copy"][1] if "copy" in big else None
+        c.mom = {k: big[k][1] for k in c.mom}
+        adamw.step(adamw.make_batch([c.tensor()]), **HYPER)
+        c.check(want)
+        for store, t in big.values():
+            assert (store[:at] == 77).all() and (store[at + t.numel():] == 77).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_from_the_start(bits):
+    """Ten steps from zero moments, eagerly and with the values on the device, against the plain form each time; and a step
+    that is skipped."""
+    rng = np.random.default_rng(8)
+    c = Case(rng, 3000, True, False, bits, copy=True)
+    c.mom = adamw.alloc_moments(c.n, bits)
+    batch = adamw.make_batch([c.tensor()])
+    live = adamw.live(0.0, 1)
+    for t in range(1, 11):
+        h = dict(lr=float(np.float32(1e-2 / t)), beta1=0.9, beta2=0.95, eps=1e-6, grad_scale=0.25, step=t)
+        c.g.copy_(torch.from_numpy(rng.normal(size=c.n).astype(np.float32)))
+        want = c.plain(h)
+        if t % 2:
+            adamw.step(batch, **h)
+        else:
+            adamw.set_live(live, h["lr"], t, h["grad_scale"])
+            adamw.step(batch, beta1=0.9, beta2=0.95, eps=1e-6, lr=-5.0, step=0, live=live)
+        c.check(want)
+    kept = [x.clone() for x in (c.w, c.copy, *(v.view(torch.uint8) if v.element_size() == 1 else v for v in c.mom.values()))]
+    adamw.set_live(live, 1.0, 11, skip=True)
+    adamw.step(batch, live=live)
+    for a, b in zip(kept, (c.w, c.copy, *(v.view(torch.uint8) if v.element_size() == 1 else v for v in c.mom.values()))):
+        assert torch.equal(a, b)
+
+
+def test_extremes():
+    """Zero gradients and moments move nothing but the decay; infinities and NaN stay in their element (32 bits) or their block
+    of 128 (8 bits); a second moment far below its block's largest keeps the smallest code instead of zero."""
+    rng = np.random.default_rng(6)
+    for bits in (32, 8):
+        c = Case(rng, 512, True, True, bits, wild=False)
+        c.mom = adamw.alloc_moments(512, bits)
+        c.g.zero_()
+        want = c.plain(HYPER)
+        adamw.step(adamw.make_batch([c.tensor()]), **HYPER)
+        c.check(want)
+        assert not c.mom["m"].float().any() and not c.mom["v"].float().any()
+        c.g.copy_(torch.from_numpy(rng.normal(size=512).astype(np.float32)))
+        c.g[5], c.g[200], c.g[300], c.g[301] = float("nan"), float("inf"), 1e-12, 1e4
+        want = c.plain(HYPER)
+        adamw.step(adamw.make_batch([c.tensor()]), **HYPER)
+        c.check(want)
+        bad = ~np.isfinite(_vals(c.mom["v"]))
+        assert bad[5] and bad[200] and not bad[256:].any()
+        if bits == 8:
+            assert _vals(c.mom["v"])[300] == 2.0 ** -9 and _vals(c.mom["m"])[300] == 0.0
+
+
+def test_offsets_behind_2_to_the_31():
+    """The last elements of a tensor of more than 2^31 of them."""
+    n = (1 << 31) + 5 * 128 + 3
+    w = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    mom = adamw.alloc_moments(n, 8)
+    rng = np.random.default_rng(2)
+    tail = 3 * 128 + 3 + 128                                  # whole blocks, from a block's first element on
+    small = Case(rng, tail, False, False, 8, wild=False)
+    small.mom = adamw.alloc_moments(tail, 8)
+    w[-tail:], g[-tail:] = small.w, small.g
+    want = small.plain(HYPER | {"lr": 0.5})
+    adamw.step(adamw.make_batch([adamw.tensor(w, g, weight_decay=small.decay, **mom)]), **(HYPER | {"lr": 0.5}))
+    assert _same(_vals(w[-tail:]), want[0]) and _same(_vals(mom["m"][-tail:]), want[1]) and _same(_vals(mom["v"][-tail:]), want[2])
+    nb = -(-tail // 128)
+    assert _same(_vals(mom["m_scale"][-nb:]), want[3][0]) and _same(_vals(mom["v_scale"][-nb:]), want[3][1])
+    assert not w[:-tail].any()
+
+
+@pytest.mark.parametrize("L", [synth.small_cases()[i] for i in (0, 2, 5, 7)], ids=lambda L: L.name)
+def test_hybrid_mask(L):
+    W, G, _ = synth.draw_small(L, 17)
+    layer = crisp.alloc_layer(desc_of(L))
+    crisp.prune_and_pack(layer, dev(W), dev(G) if G is not None else None)
+    sel = oracle.select(W, G, L.n, L.m, L.B, L.density, L.sal_kind, L.select_mode)
+    keep = np.asarray(sel.mask).reshape(L.S, L.K) != 0
+    got = adamw.hybrid_mask(layer)
+    assert (got.cpu().numpy().reshape(L.S, -1) == U.bits_of(keep)).all()
+    adamw.hybrid_mask(layer, out=layer.nm_mask)               # in place
+    assert torch.equal(layer.nm_mask, got)
+
+
+@pytest.mark.parametrize("B", [16, 32, 64])
+@pytest.mark.parametrize("topk", [0, 1])
+def test_hybrid_mask_blocks(B, topk):
+    L = synth.LayerSpec("hm", 100, 333, 8, 2, 4, B, 0.4, synth.SAL_MAG, 0.05, None, synth.LAYER_TOPK if topk else synth.ROW_UNIFORM)
+    W, G, _ = synth.draw_small(L, 3)
+    layer = crisp.alloc_layer(desc_of(L))
+    crisp.prune_and_pack(layer, dev(W), None)
+    sel = oracle.select(W, G, L.n, L.m, L.B, L.density, L.sal_kind, L.select_mode)
+    assert (adamw.hybrid_mask(layer).cpu().numpy().reshape(L.S, -1) == U.bits_of(np.asarray(sel.mask).reshape(L.S, L.K) != 0)).all()

@@ -1,0 +1,207 @@
+"""The 8-bit layers and the optimiser step where no GPU is needed: exported names, struct layouts, refusals before any device
+call, and the plain forms that the GPU tests compare with."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2311_14272_amd import adamw, crisp, fp8
+
+import lowbit_util as U
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 0x1000     # never dereferenced: the calls below fail their checks first
+
+
+def _declared(header):
+    text = open(os.path.join(ROOT, "include", header)).read()
+    return sorted(set(re.findall(r"CRISP_API[^;(]*?\b(crisp_\w+)\s*\(", text)))
+
+
+def test_headers_and_exports():
+    assert _declared("crisp_fp8.h") == ["crisp_fp8_linear", "crisp_fp8_linear_ws", "crisp_fp8_product", "crisp_fp8_quant"]
+    assert _declared("crisp_adamw.h") == ["crisp_adamw_batch", "crisp_hybrid_mask"]
+    src = '#include <stdio.h>\n#include <stddef.h>\n#include "crisp_fp8.h"\n#include "crisp_adamw.h"\nint main(void) {' \
+          'printf("%zu %zu %zu %zu %zu %zu %zu\\n", sizeof(crisp_fp8_mat), offsetof(crisp_fp8_mat, kind), sizeof(crisp_adamw_tensor),' \
+          ' offsetof(crisp_adamw_tensor, weight_decay), sizeof(crisp_adamw_hyper), offsetof(crisp_adamw_hyper, live),' \
+          ' sizeof(crisp_adamw_live)); return 0; }'
+    exe = "/tmp/crisp_lowbit_layout"
+    r = subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-x", "c", "-", "-o", exe],
+                       input=src, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    got = [int(x) for x in subprocess.run([exe], capture_output=True, text=True).stdout.split()]
+    assert got == [C.sizeof(fp8._Mat), fp8._Mat.kind.offset, C.sizeof(adamw._Tensor), adamw._Tensor.weight_decay.offset,
+                   C.sizeof(adamw._Hyper), adamw._Hyper.live.offset, 16]
+    for name in _declared("crisp_fp8.h") + _declared("crisp_adamw.h"):
+        assert getattr(crisp.lib(), name) is not None
+
+
+def _mat(R, cols_, kind_=fp8.ROWS, **k):
+    b = -(-cols_ // 128)
+    m = dict(q=FAKE, scale=FAKE, ld=b * 128, lds=R if kind_ == fp8.ROWS else b, rows=R, cols=cols_, kind=kind_, reserved=0)
+    m.update(k)
+    return fp8._Mat(**m)
+
+
+def _quant(rows=8, cols=200, X=FAKE, t=1, ldx=None, mask=None, Q="", Qt=None):
+    Q = _mat(rows, cols) if Q == "" else Q
+    return fp8.lib().crisp_fp8_quant(X, t, rows, cols, cols if ldx is None else ldx, mask, C.byref(Q) if Q else None,
+                                     C.byref(Qt) if Qt else None, None)
+
+
+def test_quant_refusals():
+    assert _quant(Q=None) == crisp.EINVAL
+    assert _quant(X=None) == crisp.EINVAL
+    assert _quant(t=2) == crisp.EINVAL
+    assert _quant(ldx=199) == crisp.ESHAPE
+    assert _quant(rows=0, Q=_mat(1, 200)) == crisp.ESHAPE
+    assert _quant(cols=0, Q=_mat(8, 1)) == crisp.ESHAPE
+    assert _quant(X=FAKE + 1) == crisp.EALIGN
+    assert _quant(X=FAKE + 2, t=0) == crisp.EALIGN
+    assert _quant(mask=FAKE + 2) == crisp.EALIGN
+    for bad, status in ((dict(q=None), crisp.EINVAL), (dict(scale=None), crisp.EINVAL), (dict(kind=2), crisp.EINVAL),
+                        (dict(reserved=1), crisp.EINVAL), (dict(ld=200), crisp.ESHAPE), (dict(ld=264), crisp.EALIGN),
+                        (dict(lds=7), crisp.ESHAPE), (dict(q=FAKE + 8), crisp.EALIGN), (dict(scale=FAKE + 2), crisp.EALIGN),
+                        (dict(rows=9, lds=9), crisp.ESHAPE), (dict(cols=201), crisp.ESHAPE), (dict(rows=-1), crisp.ESHAPE),
+                        (dict(ld=1 << 31), crisp.ESHAPE)):
+        assert _quant(Q=_mat(8, 200, **bad)) == status, bad
+    assert _quant(Qt=_mat(8, 200)) == crisp.ESHAPE                       # not the transpose
+    assert _quant(Qt=_mat(200, 8, fp8.TILES)) == crisp.EINVAL            # another kind
+    assert _quant(rows=1 << 27, cols=512, Q=_mat(1 << 27, 512)) == crisp.ESHAPE     # 2^29 blocks of a row
+
+
+def _product(X=None, W=None, Y=FAKE, ldy=64, t=1, ep=None):
+    X, W = X or _mat(16, 256), W or _mat(64, 256, fp8.TILES)
+    return fp8.lib().crisp_fp8_product(C.byref(X), C.byref(W), Y, ldy, t, C.byref(ep) if ep else None, None)
+
+
+def test_product_refusals():
+    assert _product(Y=None) == crisp.EINVAL
+    assert _product(t=2) == crisp.EINVAL
+    assert _product(X=_mat(16, 256, fp8.TILES)) == crisp.EINVAL          # X has a scale for each row
+    assert _product(W=_mat(64, 255, fp8.TILES)) == crisp.ESHAPE
+    assert _product(ldy=63) == crisp.ESHAPE
+    assert _product(Y=FAKE + 1) == crisp.EALIGN
+    assert _product(Y=FAKE + 2, t=0) == crisp.EALIGN
+    assert _product(ep=crisp.Epilogue(None, None, None, 0, 2, 0)) == crisp.EINVAL
+    assert _product(ep=crisp.Epilogue(None, None, FAKE, 63, 0, 0)) == crisp.ESHAPE
+    assert _product(ep=crisp.Epilogue(None, None, FAKE, 72, 0, 0)) == crisp.ESHAPE      # Y itself with another row length
+    assert _product(ep=crisp.Epilogue(FAKE + 2, None, None, 0, 0, 0)) == crisp.EALIGN
+    assert _product(X=_mat(1 << 20, 256), W=_mat(1 << 20, 256, fp8.TILES), ldy=1 << 20) == crisp.ESHAPE   # 2^32 tiles
+    L = fp8.lib()
+    assert L.crisp_fp8_product(None, None, FAKE, 64, 1, None, None) == crisp.EINVAL
+
+
+def test_linear_refusals():
+    L = fp8.lib()
+    need = L.crisp_fp8_linear_ws(16, 200)
+    assert need == 16 * (256 + 2 * 4)
+    assert L.crisp_fp8_linear_ws(0, 200) == 0 and L.crisp_fp8_linear_ws(16, -1) == 0 and L.crisp_fp8_linear_ws(1 << 27, 512) == 0
+    W = _mat(64, 200, fp8.TILES)
+
+    def linear(X=FAKE, t=1, T=16, ldx=200, Y=FAKE, ldy=64, ws=FAKE, n=need):
+        return L.crisp_fp8_linear(X, t, T, ldx, C.byref(W), Y, ldy, 1, None, ws, n, None)
+    assert linear(X=None) == crisp.EINVAL and linear(Y=None) == crisp.EINVAL and linear(t=7) == crisp.EINVAL
+    assert linear(T=0) == crisp.ESHAPE and linear(ldx=199) == crisp.ESHAPE and linear(ldy=63) == crisp.ESHAPE
+    assert linear(ws=FAKE + 8) == crisp.EALIGN
+    assert linear(ws=None) == crisp.EBUFSIZE and linear(n=need - 1) == crisp.EBUFSIZE
+    assert L.crisp_fp8_linear(FAKE, 1, 16, 200, None, FAKE, 64, 1, None, FAKE, need, None) == crisp.EINVAL
+
+
+def _adamw(h=None, count=1, **k):
+    t = dict(w=FAKE, g=FAKE, m=FAKE, v=FAKE, m_scale=None, v_scale=None, w_copy=None, mask=None, numel=1000, row_len=0, w_type=0,
+             g_type=0, moments=0, weight_decay=0.0)
+    t.update(k)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, step=1, live=None)
+    hyper.update(h or {})
+    # the first tensor has no elements, so that nothing would be enqueued for it
+    arr = (adamw._Tensor * 2)(adamw._Tensor(**{**t, "numel": 0, "w": None}), adamw._Tensor(**t))
+    return adamw.lib().crisp_adamw_batch(count + 1 if count > 0 else count, arr, C.byref(adamw._Hyper(**hyper)), None)
+
+
+def test_adamw_refusals():
+    for k in ("w", "g", "m", "v"):
+        assert _adamw(**{k: None}) == crisp.EINVAL
+        assert _adamw(**{k: FAKE + 8}) == crisp.EALIGN
+    assert _adamw(count=0) == crisp.EINVAL and _adamw(count=1 << 20) == crisp.EINVAL
+    for bad in (dict(w_type=2), dict(g_type=-1), dict(moments=2), dict(weight_decay=-0.1), dict(weight_decay=float("nan")),
+                dict(moments=1), dict(moments=1, m_scale=FAKE), dict(m_scale=FAKE), dict(w_type=1, w_copy=FAKE)):
+        assert _adamw(**bad) == crisp.EINVAL, bad
+    for bad in (dict(numel=-1), dict(mask=FAKE), dict(mask=FAKE, row_len=300), dict(mask=FAKE, row_len=1, numel=1 << 31),
+                dict(numel=1 << 40)):
+        assert _adamw(**bad) == crisp.ESHAPE, bad
+    assert _adamw(moments=1, m_scale=FAKE + 2, v_scale=FAKE) == crisp.EALIGN
+    assert _adamw(mask=FAKE + 1, row_len=10) == crisp.EALIGN and _adamw(w_copy=FAKE + 2) == crisp.EALIGN
+    for bad in (dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(lr=-1.0), dict(lr=float("nan")), dict(step=0),
+                dict(step=1 << 31), dict(grad_scale=float("inf"))):
+        assert _adamw(h=bad) == crisp.EINVAL, bad
+    assert _adamw(h=dict(live=FAKE + 2)) == crisp.EALIGN
+    assert adamw.lib().crisp_adamw_batch(1, None, None, None) == crisp.EINVAL
+
+
+def test_hybrid_mask_refusals():
+    L = adamw.lib()
+    d = crisp.layer_desc(64, 128, 2, 4, 32, 0.5)
+    assert L.crisp_hybrid_mask(C.byref(d), None, FAKE, FAKE, FAKE, None) == crisp.EINVAL
+    assert L.crisp_hybrid_mask(C.byref(d), FAKE, FAKE, FAKE, FAKE + 2, None) == crisp.EALIGN
+    assert L.crisp_hybrid_mask(None, FAKE, FAKE, FAKE, FAKE, None) == crisp.EINVAL
+    assert L.crisp_hybrid_mask(C.byref(crisp.layer_desc(0, 128, 2, 4, 32, 0.5)), FAKE, FAKE, FAKE, FAKE, None) == crisp.ESHAPE
+
+
+def test_tensors_off_the_gpu_are_refused():
+    x = torch.zeros(4, 128)
+    with pytest.raises((ValueError, RuntimeError)):      # (without any GPU there is no current one to compare with)
+        fp8.Fp8Mat(torch.zeros((4, 128), dtype=torch.uint8), torch.zeros((1, 4)), 4, 128, fp8.ROWS)
+    with pytest.raises(ValueError):
+        fp8.Fp8Mat(torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((1, 4)), 4, 128, fp8.ROWS)
+    with pytest.raises(ValueError):
+        fp8.quantize(x.to(torch.float64), out=object())
+    with pytest.raises(ValueError):
+        adamw.tensor(x, x, x, x.double())
+    with pytest.raises(ValueError):
+        adamw.tensor(x, x, x, x, m_scale=torch.zeros(4))
+    with pytest.raises(ValueError):
+        adamw.tensor(x.t(), x, x, x)
+    with pytest.raises(ValueError):
+        adamw.make_batch([])
+
+
+def test_plain_e4m3_rounding():
+    """All 256 codes stand for themselves; values between two neighbours go to the nearer one, the middle to the even one."""
+    codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
+    fine = codes[np.isfinite(codes)]
+    assert fine.max() == 448.0 and (U.e4m3(fine) == fine).all()
+    pos = np.unique(fine[fine >= 0])
+    mid = (pos[1:] + pos[:-1]) / 2
+    even = np.where(np.arange(mid.size) % 2 == 0, pos[:-1], pos[1:])
+    assert (U.e4m3(mid) == even).all() and (U.e4m3(-mid) == -even).all()
+    assert (U.e4m3(mid * (1 - 1e-9)) == pos[:-1]).all() and (U.e4m3(mid * (1 + 1e-9)) == pos[1:]).all()
+    assert U.e4m3(450.0) == 448.0 and np.isnan(U.e4m3(np.nan)) and np.isnan(U.e4m3(np.inf))
+
+
+def test_plain_step_against_64_bits():
+    """The fp32 form of the step that the kernels are held to, against the same formulas in 64 bits.
+    In units of 2^-24: m carries the roundings of beta1 (or 1 - beta1), g', the product and the sum, 4; v of 1 - beta2, twice g',
+    its square, the product and the sum, 6; the root half of that and its own, 4; the denominator the correction's, the product's,
+    the sum's, 7; the quotient 8 and m's 4, on M = |beta1 m| + |(1 - beta1) g'|; the step's rounded size, product and the
+    difference 3 more; the weight its factor, product and difference, 3."""
+    rng = np.random.default_rng(3)
+    n, lr, b1, b2, eps, gs, step, decay = 5000, 1e-3, 0.9, 0.999, 1e-8, 0.25, 7, 0.1
+    w, g = rng.normal(size=n).astype(U.F), (rng.normal(size=n) * 10.0 ** rng.uniform(-9, 2, n)).astype(U.F)
+    m, v = (rng.normal(size=n) * np.abs(g) * 0.3).astype(U.F), (g * g * rng.uniform(0, 2, n)).astype(U.F)
+    nw, nm, nv, _ = U.adamw(w, g, m, v, None, lr, b1, b2, eps, gs, step, decay)
+    W, G, M, V = (a.astype(np.float64) for a in (w, g, m, v))
+    G = G * gs
+    em, ev = b1 * M + (1 - b1) * G, b2 * V + (1 - b2) * G * G
+    den = np.sqrt(ev / (1 - b2 ** step)) + eps
+    ew = W - lr * decay * W - lr / (1 - b1 ** step) * em / den
+    h, tiny = 2.0 ** -24 * 1.01, 1e-44
+    size = np.abs(b1 * M) + np.abs((1 - b1) * G)
+    assert (np.abs(nm - em) <= 4 * h * size + tiny).all()
+    assert (np.abs(nv - ev) <= 6 * h * ev + 4 * tiny).all()
+    fine = ev > 1e-36          # (where the second moment is subnormal its roundings are not relative)
+    assert (np.abs(nw - ew) <= 3 * h * np.abs(W) + 15 * h * lr / (1 - b1 ** step) * size / den + 1e-30)[fine].all()
