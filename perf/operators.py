@@ -188,7 +188,7 @@ def prepare(case, seed):
     if own:
         from paper_2311_14272_amd import fp8
         for k, rows, cols, how in names:
-            st[k] = fp8.Fp8Mat(st[k][0], st[k][1], rows, cols, how)
+            st[k] = fp8.Fp8Mat(st[k][0].contiguous(), st[k][1], rows, cols, how)
     return st
 
 
