@@ -125,7 +125,8 @@ def _pair(seed, T, S, K, w_tiles):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 128), (2, 48, 100), (1, 1000, 4096), (5, 130, 640), (16, 128, 1152), (17, 33, 257), (31, 520, 2050),
             (48, 64, 8192), (64, 4096, 256), (65, 200, 384), (100, 129, 1000), (128, 128, 128), (129, 300, 512), (255, 257, 300),
-            (256, 256, 256), (333, 1000, 130), (512, 512, 1152), (700, 384, 2304), (1030, 1025, 140)]
+            (256, 256, 256), (333, 1000, 130), (512, 512, 1152), (700, 384, 2304), (1030, 1025, 140),
+            (3400, 3841, 260), (4096, 4096, 128)]
 
 
 @pytest.mark.parametrize("w_tiles", [True, False], ids=["tiles", "rows"])
