@@ -19,7 +19,10 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 constexpr int GROUP = 4;
 constexpr int XCDS = 8;
 
-__device__ __forceinline__ int w_swizzle(int r) { return (r & 3) | ((r >> 2) & 4); }
+// Chunk c of row r lies at place c ^ swizzle(r).  A read serves 16 lanes a cycle from 64 banks of 4 bytes, two rows' worth: of
+// the 16 rows that those lanes want, the eight of either parity have different values here.
+__device__ __forceinline__ int x_swizzle(int r) { return (r >> 1) & 7; }                       // rows 16n .. 16n+15
+__device__ __forceinline__ int w_swizzle(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }    // 8m+{0..7}, 8m+16+{0..7}
 
 // Sixteen consecutive results of row t from column s on.
 template <bool BF16>
@@ -42,13 +45,30 @@ __device__ __forceinline__ void store_y16(const ProductArgs& a, int t, int s, co
         if (s + j < a.S) store_y(a, t, s + j, v[j]);
 }
 
-// NS x NT waves, each RS x RT tiles of 32 x 32.  BF16: the result's type, and with it the instruction.  TILES: W's scales.
-template <int NS, int NT, int RS, int RT, bool BF16, bool TILES>
-__global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
+// Waits until at most `left` of the wave's memory operations are outstanding, and for all its LDS reads.
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(LEFT < 64, "six bits");
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | 0 << 8 | (LEFT >> 4) << 14);
+}
+
+// NS x NT waves, each RS x RT tiles of 32 x 32; STAGES blocks in LDS, all but one of them on their way.  BF16: the result's
+// type, and with it the instruction.  TILES: W has a scale for 128 x 128, one for all of a wave's rows.
+//
+// A step begins when its block has arrived for every wave (each waits for its own share, then all meet) - by then everybody
+// is done with the block before, whose place the next request takes.  All a wave's memory operations are requests to LDS,
+// the same number each step, so that the wait can leave the later steps' ones outstanding.
+template <int NS, int NT, int RS, int RT, int STAGES, bool BF16, bool TILES>
+__global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
     constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
-    constexpr int LW = BS / 8 / NW, LX = BT / 8 / NW;            // loads of eight rows that a wave issues
-    __shared__ __align__(16) uint8_t w_even[BS * 128], w_odd[BS * 128], x_even[BT * 128], x_odd[BT * 128];
-    __shared__ __align__(16) float s_even[TILES ? 4 : BS], s_odd[TILES ? 4 : BS];
+    constexpr int LW = BS / 8 / NW, LX = BT / 8 / NW;            // requests of eight rows that a wave makes per step
+    constexpr int LS = ((BS + BT) / 64 + NW - 1) / NW;           // and of 64 scales (some may be nobody's)
+    constexpr int SC = LS * NW * 64;
+    static_assert(BS % (8 * NW) == 0 && BT % (8 * NW) == 0 && BS % 64 == 0, "whole requests");
+    constexpr int PER = LW + LX + LS;
+    __shared__ __align__(16) uint8_t w0[BS * 128], x0[BT * 128], w1[BS * 128], x1[BT * 128];
+    __shared__ __align__(16) uint8_t w2[STAGES > 2 ? BS * 128 : 16], x2[STAGES > 2 ? BT * 128 : 16], w3[STAGES > 3 ? BS * 128 : 16], x3[STAGES > 3 ? BT * 128 : 16];
+    __shared__ __align__(16) float s0_[SC], s1_[SC], s2_[STAGES > 2 ? SC : 4], s3_[STAGES > 3 ? SC : 4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 
     int id = blockIdx.x;
@@ -68,9 +88,24 @@ __global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_
 #pragma unroll
     for (int j = 0; j < LX; ++j) {
         const int r = (wave + j * NW) * 8 + lane / 8;
-        xo[j] = (uint32_t)min(r, a.T - 1 - t0) * (uint32_t)a.ldx + (lane % 8 ^ r % 8) * 16;
+        xo[j] = (uint32_t)min(r, a.T - 1 - t0) * (uint32_t)a.ldx + (lane % 8 ^ x_swizzle(r)) * 16;
     }
     const uint8_t *wb = a.w + s0 * a.ldw, *xb = a.x + t0 * a.ldx;
+    // scales: a wave's 64 rows are W's or X's
+    const float* sp[LS];
+    int64_t sstep[LS];
+#pragma unroll
+    for (int j = 0; j < LS; ++j) {
+        const int r = (wave + j * NW) * 64 + lane;
+        if ((wave + j * NW) * 64 < BS) {
+            const int row = min(s0 + r, a.S - 1);
+            sp[j] = a.ws + (a.w_tiles ? row / 128 * a.ldws : (int64_t)row);
+            sstep[j] = a.w_tiles ? 1 : a.ldws;
+        } else {
+            sp[j] = a.xs + min(t0 + r - BS, a.T - 1);
+            sstep[j] = a.ldxs;
+        }
+    }
 
     const int i = lane % 32, h = lane / 32;
     const int ws = wave % NS, wt = wave / NS;
@@ -79,12 +114,8 @@ __global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         wr[c] = (ws * RS * 32 + si) * 128 + ((4 * h + c) ^ w_swizzle(si)) * 16;
-        xr[c] = (wt * RT * 32 + i) * 128 + ((4 * h + c) ^ (i & 7)) * 16;
+        xr[c] = (wt * RT * 32 + i) * 128 + ((4 * h + c) ^ x_swizzle(i)) * 16;
     }
-    int tcol[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) tcol[r] = min(t0 + (wt * RT + r) * 32 + i, a.T - 1);
-    const float* wscale = a.ws + (TILES ? (int64_t)min((s0 + ws * RS * 32) / 128, (a.S - 1) / 128) * a.ldws : 0);
 
     f32x16 acc[RS][RT];
 #pragma unroll
@@ -93,32 +124,41 @@ __global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_
         for (int q = 0; q < RT; ++q)
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][q][j] = 0.0f;
-    float next[RT], wnext = 0.0f;
 
+    // request n of a step's PER
+    auto request = [&](int n, int b, uint8_t* wl, uint8_t* xl, float* sl) {
+        if (n < LS) {
+            const int j = n;
+            __builtin_amdgcn_global_load_lds((global_ptr)(sp[j] + b * sstep[j]), (lds_ptr)(sl + (wave + j * NW) * 64), 4, 0, 0);
+        } else if (n < LS + LW) {
+            const int j = n - LS;
+            __builtin_amdgcn_global_load_lds((global_ptr)(wb + (int64_t)b * 128 + wo[j]), (lds_ptr)(wl + (wave + j * NW) * 1024), 16, 0, 0);
+        } else {
+            const int j = n - LS - LW;
+            __builtin_amdgcn_global_load_lds((global_ptr)(xb + (int64_t)b * 128 + xo[j]), (lds_ptr)(xl + (wave + j * NW) * 1024), 16, 0, 0);
+        }
+    };
     auto fetch = [&](int b, uint8_t* wl, uint8_t* xl, float* sl) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) next[r] = a.xs[b * a.ldxs + tcol[r]];
-        if constexpr (TILES) {
-            wnext = wscale[b];
-        } else {
-            if (wave < BS / 64) {
-                const int row = min(s0 + wave * 64 + lane, a.S - 1);
-                __builtin_amdgcn_global_load_lds((global_ptr)(a.ws + b * a.ldws + row), (lds_ptr)(sl + wave * 64), 4, 0, 0);
-            }
-        }
-        const uint8_t *wp = wb + (int64_t)b * 128, *xp = xb + (int64_t)b * 128;
-#pragma unroll
-        for (int j = 0; j < LW; ++j) __builtin_amdgcn_global_load_lds((global_ptr)(wp + wo[j]), (lds_ptr)(wl + (wave + j * NW) * 1024), 16, 0, 0);
-#pragma unroll
-        for (int j = 0; j < LX; ++j) __builtin_amdgcn_global_load_lds((global_ptr)(xp + xo[j]), (lds_ptr)(xl + (wave + j * NW) * 1024), 16, 0, 0);
+        for (int n = 0; n < PER; ++n) request(n, b, wl, xl, sl);
     };
 
-    auto compute = [&](const uint8_t* wl, const uint8_t* xl, const float* sl, const float (&f)[RT]) {
-        i32x4 xv[RT][4];
+    auto compute = [&](const uint8_t* wl, const uint8_t* xl, const float* sl, auto part) {
+        i32x4 xv[RT][4], wv[4];
+        float f[RT];
 #pragma unroll
-        for (int q = 0; q < RT; ++q)
+        for (int c = 0; c < 4; ++c) {
+            wv[c] = *reinterpret_cast<const i32x4*>(wl + wr[c]);
+            xv[0][c] = *reinterpret_cast<const i32x4*>(xl + xr[c]);
+        }
+#pragma unroll
+        for (int q = 1; q < RT; ++q)
 #pragma unroll
             for (int c = 0; c < 4; ++c) xv[q][c] = *reinterpret_cast<const i32x4*>(xl + xr[c] + q * 4096);
+#pragma unroll
+        for (int q = 0; q < RT; ++q) f[q] = sl[BS + (wt * RT + q) * 32 + i];
+        const float wscale = TILES ? sl[ws * RS * 32] : 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
         bf16x8 xw[BF16 ? 1 : RT][8];
         if constexpr (!BF16) {
 #pragma unroll
@@ -129,61 +169,82 @@ __global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_
                     xw[q][2 * c + 1] = widen(xv[q][c][2], xv[q][c][3]);
                 }
         }
+        f32x16 p[2];
+        f32x4 wsv[4];
+        const f32x16 zero = {};
+        // the matrix cores are a tile ahead of the sums that enter the accumulators
 #pragma unroll
-        for (int r = 0; r < RS; ++r) {
-            i32x4 wv[4];
+        for (int k = 0; k <= RS * RT; ++k) {
+            if (k < RS * RT) {
+                const int r = k / RT, q = k % RT;
+                if constexpr (BF16) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) wv[c] = *reinterpret_cast<const i32x4*>(wl + wr[c] + r * 4096);
-            f32x4 wsv[4];
-            if constexpr (!TILES) {
+                    for (int u = 0; u < 2; ++u) {
+                        const i32x8 wa = __builtin_shufflevector(wv[2 * u], wv[2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        const i32x8 xa = __builtin_shufflevector(xv[q][2 * u], xv[q][2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        p[k % 2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, xa, u ? p[k % 2] : zero, 0, 0, 0, 0, 0, 0);
+                    }
+                } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(sl + (ws * RS + r) * 32 + 16 * h + 4 * c);
-            }
-            f32x16 p[RT];
-            const f32x16 zero = {};
-            if constexpr (BF16) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const i32x8 wa = __builtin_shufflevector(wv[2 * k], wv[2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-                    for (int q = 0; q < RT; ++q) {
-                        const i32x8 xa = __builtin_shufflevector(xv[q][2 * k], xv[q][2 * k + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-                        p[q] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, xa, k ? p[q] : zero, 0, 0, 0, 0, 0, 0);
+                    for (int u = 0; u < 8; ++u) {
+                        const bf16x8 wa = widen(wv[u / 2][u % 2 * 2], wv[u / 2][u % 2 * 2 + 1]);
+                        p[k % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, xw[q][u], u ? p[k % 2] : zero, 0, 0, 0);
                     }
                 }
-            } else {
+                __builtin_amdgcn_sched_barrier(0);
+                if (TILES && k == 0) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const bf16x8 wa = widen(wv[k / 2][k % 2 * 2], wv[k / 2][k % 2 * 2 + 1]);
-#pragma unroll
-                    for (int q = 0; q < RT; ++q) p[q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, xw[q][k], k ? p[q] : zero, 0, 0, 0);
+                    for (int e = 0; e < RT; ++e) f[e] *= wscale;
                 }
+                if (q == RT - 1 && r + 1 < RS) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) wv[c] = *reinterpret_cast<const i32x4*>(wl + wr[c] + (r + 1) * 4096);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                part(k);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            if (k > 0) {
+                const int r = (k - 1) / RT, q = (k - 1) % RT;
+                if (!TILES && q == 0) {
 #pragma unroll
-            for (int q = 0; q < RT; ++q)
+                    for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(sl + (ws * RS + r) * 32 + 16 * h + 4 * c);
+                }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[q][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
+                for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
 
-    float f[RT];
-    auto take = [&]() {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) f[r] = TILES ? next[r] * wnext : next[r];
-    };
-    fetch(0, w_even, x_even, s_even);
-    __syncthreads();
-    for (int b = 0; b < a.kb; b += 2) {
-        take();
-        if (b + 1 < a.kb) fetch(b + 1, w_odd, x_odd, s_odd);
-        compute(w_even, x_even, s_even, f);
-        __syncthreads();
-        if (b + 1 >= a.kb) break;
-        take();
-        if (b + 2 < a.kb) fetch(b + 2, w_even, x_even, s_even);
-        compute(w_odd, x_odd, s_odd, f);
-        __syncthreads();
+    constexpr int AHEAD = STAGES - 1;
+    constexpr int SPREAD = STAGES == 2 ? (RS * RT + 1) / 2 : RS * RT;     // tiles of a step that its requests go between
+    // (behind the last block the requests repeat it, into places that nobody reads any more: a step is then free of branches)
+#define CRISP_STEP(k, here, there)                                                                                \
+    {                                                                                                             \
+        const int b = b0 + k, ahead = min(b + AHEAD, a.kb - 1);                                                   \
+        wait_loads<(AHEAD - 1) * PER>();                                                                          \
+        __builtin_amdgcn_s_barrier();                                                                             \
+        compute(w##here, x##here, s##here##_, [&](int tile) {                                                     \
+            _Pragma("unroll") for (int n = 0; n < PER; ++n)                                                       \
+                if (n * SPREAD / PER == tile) request(n, ahead, w##there, x##there, s##there##_);                \
+        });                                                                                                       \
+        if (b + 1 >= a.kb) break;                                                                                 \
     }
+    fetch(0, w0, x0, s0_);
+    if constexpr (AHEAD > 1) fetch(min(1, a.kb - 1), w1, x1, s1_);
+    if constexpr (AHEAD > 2) fetch(min(2, a.kb - 1), w2, x2, s2_);
+    for (int b0 = 0;; b0 += STAGES) {
+        if constexpr (STAGES == 2) {
+            CRISP_STEP(0, 0, 1) CRISP_STEP(1, 1, 0)
+        } else if constexpr (STAGES == 3) {
+            CRISP_STEP(0, 0, 2) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1)
+        } else {
+            CRISP_STEP(0, 0, 3) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1) CRISP_STEP(3, 3, 2)
+        }
+    }
+#undef CRISP_STEP
+    wait_loads<0>();
 
     const bool plain = !a.scale && !a.bias && !a.residual && !a.relu && ((uintptr_t)a.y & 15) == 0 && a.ldy % (BF16 ? 8 : 4) == 0;
 #pragma unroll
@@ -193,21 +254,27 @@ __global__ __launch_bounds__(64 * NS * NT, NS * NT == 8 ? 2 : 2) void fp8_tiled_
             store_y16<BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, acc[r][q], plain);
 }
 
-template <int NS, int NT, int RS, int RT, bool BF16>
+template <int NS, int NT, int RS, int RT, int STAGES, bool BF16>
 static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + NS * RS * 32 - 1) / (NS * RS * 32), tt = (a.T + NT * RT * 32 - 1) / (NT * RT * 32);
-    const unsigned grid = (unsigned)ts * (unsigned)tt;
-    if (a.w_tiles) fp8_tiled_kernel<NS, NT, RS, RT, BF16, true><<<grid, 64 * NS * NT, 0, st>>>(a, ts, tt);
-    else fp8_tiled_kernel<NS, NT, RS, RT, BF16, false><<<grid, 64 * NS * NT, 0, st>>>(a, ts, tt);
+    auto kernel = a.w_tiles ? fp8_tiled_kernel<NS, NT, RS, RT, STAGES, BF16, true> : fp8_tiled_kernel<NS, NT, RS, RT, STAGES, BF16, false>;
+    kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT, 0, st>>>(a, ts, tt);
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
     const int64_t big = (int64_t)((a.S + 255) / 256) * ((a.T + 255) / 256);
+    const int64_t mid = (int64_t)((a.S + 127) / 128) * ((a.T + 127) / 128);
     // 256 x 256 tiles where they fill three quarters of the CUs.  Widening to bf16 takes more registers than such a wave has
     // left: 128 x 128 for fp32 results (4096 x 4096 x 4096: 660 TFLOP/s with 256 x 256, 980 at half the rows with 128 x 128).
-    if (a.y_bf16 && big >= 192) launch_tiles<2, 4, 4, 2, true>(a, st);
-    else if (a.y_bf16) launch_tiles<2, 2, 2, 2, true>(a, st);
-    else launch_tiles<2, 2, 2, 2, false>(a, st);
+    if (a.y_bf16) {
+        if (big >= 192 && a.w_tiles) launch_tiles<2, 4, 4, 2, 2, true>(a, st);
+        else if (mid > 256) launch_tiles<2, 2, 2, 2, 2, true>(a, st);
+        else if (mid >= 192) launch_tiles<2, 2, 2, 2, 4, true>(a, st);
+        else launch_tiles<2, 2, 2, 1, 4, true>(a, st);
+    } else {
+        if (mid >= 192) launch_tiles<2, 2, 2, 2, 2, false>(a, st);
+        else launch_tiles<2, 2, 2, 1, 4, false>(a, st);
+    }
     return hipGetLastError();
 }
 
