@@ -11,7 +11,7 @@ OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["spmm_nm_2_4.hip", "spmm_nm_4_8.hip", "spmm_nm_3_4.hip", "spmm_nm_4_4.hip", "spmm_nm_8_8.hip", "spmm_nm_1_4.hip",
            "spmm_nm_2_8.hip", "spmm_nm_1_8.hip", "spmm_lds.hip", "spmm_kernels.hip", "crisp_api.hip", "select_kernels.hip",
-           "pack_kernels.hip", "im2col_kernels.hip", "budget_kernels.hip", "fp8_quant.hip", "fp8_product.hip", "fp8_tiled.hip", "fp8_api.hip",
+           "pack_kernels.hip", "im2col_kernels.hip", "budget_kernels.hip", "fp8_quant.hip", "fp8_product.hip", "fp8_tiled.hip", "fp8_split.hip", "fp8_api.hip",
            "adamw.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-ffp-contract=off",

@@ -24,13 +24,15 @@ static crisp_status check_mat(const crisp_fp8_mat* m) {
 // A launch takes fewer than 2^32 threads: 16 of them for a block of 128 columns.
 static bool too_many(int64_t rows, int64_t cols) { return rows * blocks(cols) > ((int64_t)1 << 28) - 16; }
 
-static crisp_status check_out(const void* Y, int64_t T, int64_t S, int64_t ldy, int32_t y_type, const crisp_epilogue* ep) {
+static crisp_status check_out(const void* Y, int64_t T, int64_t S, int64_t most_ld, int64_t ldy, int32_t y_type, const crisp_epilogue* ep) {
     if (!Y) return CRISP_EINVAL;
     if (y_type != CRISP_Y_F32 && y_type != CRISP_Y_BF16) return CRISP_EINVAL;
     if (ldy < S || ldy > MOST_LD) return CRISP_ESHAPE;
     const size_t size = y_type == CRISP_Y_BF16 ? 2 : 4;
     if (off(Y, size)) return CRISP_EALIGN;
-    if (((T + 15) / 16) * ((S + 15) / 16) > ((int64_t)1 << 26) - 4) return CRISP_ESHAPE;   // 64 threads for 16 x 16 outputs
+    // a launch takes fewer than 2^32 threads: 512 for 16 x 16 results at least, or for 64 x 64
+    const int64_t tiles = ((T + 15) / 16) * ((S + 15) / 16);
+    if (tiles > (fp8_takes_split(T, S, most_ld) ? ((int64_t)1 << 23) - 1 : ((int64_t)1 << 26))) return CRISP_ESHAPE;
     if (!ep) return CRISP_OK;
     if (ep->relu != 0 && ep->relu != 1) return CRISP_EINVAL;
     if (ep->residual && (ep->ldr < S || ep->ldr > MOST_LD)) return CRISP_ESHAPE;
@@ -72,7 +74,7 @@ crisp_status crisp_fp8_product(const crisp_fp8_mat* X, const crisp_fp8_mat* W, v
     if (st != CRISP_OK || (st = check_mat(W)) != CRISP_OK) return st;
     if (X->kind != CRISP_FP8_ROWS) return CRISP_EINVAL;
     if (X->cols != W->cols) return CRISP_ESHAPE;
-    if ((st = check_out(Y, X->rows, W->rows, ldy, y_type, ep)) != CRISP_OK) return st;
+    if ((st = check_out(Y, X->rows, W->rows, X->ld > W->ld ? X->ld : W->ld, ldy, y_type, ep)) != CRISP_OK) return st;
     return launch_fp8_product(*X, *W, Y, ldy, y_type, ep, (hipStream_t)stream) == hipSuccess ? CRISP_OK : CRISP_EDEVICE;
 }
 
@@ -86,7 +88,7 @@ crisp_status crisp_fp8_linear(const void* X, int32_t in_type, int64_t T, int64_t
     if (!W) return CRISP_EINVAL;
     crisp_status st = check_mat(W);
     if (st != CRISP_OK || (st = check_in(X, in_type, T, W->cols, ldx)) != CRISP_OK) return st;
-    if ((st = check_out(Y, T, W->rows, ldy, y_type, ep)) != CRISP_OK) return st;
+    if ((st = check_out(Y, T, W->rows, W->ld, ldy, y_type, ep)) != CRISP_OK) return st;
     if (off(ws, 16)) return CRISP_EALIGN;
     if (!ws || ws_bytes < crisp_fp8_linear_ws(T, W->cols)) return CRISP_EBUFSIZE;
     const int64_t ld = blocks(W->cols) * FP8_BLOCK;

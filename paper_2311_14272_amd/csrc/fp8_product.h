@@ -54,5 +54,6 @@ __device__ __forceinline__ void store_y(const ProductArgs& a, int64_t t, int s, 
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st);
+hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st);
 
 }  // namespace crisp

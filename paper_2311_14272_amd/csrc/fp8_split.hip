@@ -1,0 +1,142 @@
+// The 8-bit product for few rows of X: the weights are read once and bound it, so nothing is staged.  A workgroup computes
+// 16 MS x 16 MT results (W rows x X rows); its waves take the blocks of 128 columns in turn, straight from memory into the
+// matrix instruction's registers, and add their sums up in LDS, in the order of the waves.
+//
+// Lane l holds 32 columns of row l % 16 of either operand, the same ones of both, so that their order does not matter;
+// register i of lane l is (W row 4 (l / 16) + i, X row l % 16).
+#include "fp8_product.h"
+
+namespace crisp {
+
+constexpr int SPLIT_WAVES = 8;
+
+template <bool BF16>
+__device__ __forceinline__ f32x4 block_sum(const i32x4 (&w)[2], const i32x4 (&x)[2]) {
+    f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (BF16) {
+        const i32x8 wa = __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        const i32x8 xa = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wa, xa, c, 0, 0, 0, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[k / 2][k % 2 * 2], w[k / 2][k % 2 * 2 + 1]),
+                                                        widen(x[k / 2][k % 2 * 2], x[k / 2][k % 2 * 2 + 1]), c, 0, 0, 0);
+        return c;
+    }
+}
+
+// U: blocks that a wave requests at a time.
+template <int MS, int MT, int U, bool BF16, bool TILES>
+__global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs a, int tiles_s) {
+    __shared__ f32x4 part[SPLIT_WAVES][MS * MT][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int i = lane % 16, h = lane / 16;
+    const int s0 = (int)(blockIdx.x % tiles_s) * (16 * MS), t0 = (int)(blockIdx.x / tiles_s) * (16 * MT);
+    // rows behind the last one repeat it, their results are not stored
+    const uint8_t *w[MS], *x[MT];
+    const float* xs[MT];
+    const float* wsp[MS];
+#pragma unroll
+    for (int r = 0; r < MS; ++r) {
+        w[r] = a.w + min(s0 + 16 * r + i, a.S - 1) * a.ldw + h * 32;
+        wsp[r] = TILES ? a.ws + min(s0 + 16 * r, a.S - 1) / 128 * a.ldws : a.ws;
+    }
+#pragma unroll
+    for (int q = 0; q < MT; ++q) {
+        const int t = min(t0 + 16 * q + i, a.T - 1);
+        x[q] = a.x + t * a.ldx + h * 32;
+        xs[q] = a.xs + t;
+    }
+    f32x4 sum[MS][MT];
+#pragma unroll
+    for (int r = 0; r < MS; ++r)
+#pragma unroll
+        for (int q = 0; q < MT; ++q) sum[r][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    for (int b0 = wave; b0 < a.kb; b0 += U * SPLIT_WAVES) {
+        i32x4 wv[U][MS][2], xv[U][MT][2];
+        float f[U][MT], g[U][MS][TILES ? 1 : 4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = min(b0 + u * SPLIT_WAVES, a.kb - 1);       // (behind the last block it is fetched again and left out)
+#pragma unroll
+            for (int r = 0; r < MS; ++r) {
+                wv[u][r][0] = *reinterpret_cast<const i32x4*>(w[r] + (int64_t)b * 128);
+                wv[u][r][1] = *reinterpret_cast<const i32x4*>(w[r] + (int64_t)b * 128 + 16);
+                if constexpr (TILES) {
+                    g[u][r][0] = wsp[r][b];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) g[u][r][j] = a.ws[b * a.ldws + min(s0 + 16 * r + 4 * h + j, a.S - 1)];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < MT; ++q) {
+                xv[u][q][0] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128);
+                xv[u][q][1] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128 + 16);
+                f[u][q] = xs[q][b * a.ldxs];
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);       // all requests first
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool there = b0 + u * SPLIT_WAVES < a.kb;
+#pragma unroll
+            for (int r = 0; r < MS; ++r)
+#pragma unroll
+                for (int q = 0; q < MT; ++q) {
+                    const f32x4 p = block_sum<BF16>(wv[u][r], xv[u][q]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float next = __builtin_fmaf(p[j], f[u][q] * g[u][r][TILES ? 0 : j], sum[r][q][j]);
+                        sum[r][q][j] = there ? next : sum[r][q][j];
+                    }
+                }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < MS; ++r)
+#pragma unroll
+        for (int q = 0; q < MT; ++q) part[wave][r * MT + q][lane] = sum[r][q];
+    __syncthreads();
+    // thread (tile, lane): four consecutive results of a row
+    for (int e = threadIdx.x; e < MS * MT * 64; e += 64 * SPLIT_WAVES) {
+        const int tile = e / 64, l = e % 64;
+        f32x4 y = part[0][tile][l];
+#pragma unroll
+        for (int v = 1; v < SPLIT_WAVES; ++v) y += part[v][tile][l];
+        const int t = t0 + tile % MT * 16 + l % 16, s = s0 + tile / MT * 16 + l / 16 * 4;
+        if (t < a.T) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (s + j < a.S) store_y(a, t, s + j, y[j]);
+        }
+    }
+}
+
+template <int MS, int MT, int U>
+static void launch_split(const ProductArgs& a, hipStream_t st) {
+    const int ts = (a.S + 16 * MS - 1) / (16 * MS), tt = (a.T + 16 * MT - 1) / (16 * MT);
+    auto kernel = a.y_bf16 ? (a.w_tiles ? fp8_split_kernel<MS, MT, U, true, true> : fp8_split_kernel<MS, MT, U, true, false>)
+                           : (a.w_tiles ? fp8_split_kernel<MS, MT, U, false, true> : fp8_split_kernel<MS, MT, U, false, false>);
+    kernel<<<(unsigned)ts * (unsigned)tt, 64 * SPLIT_WAVES, 0, st>>>(a, ts);
+}
+
+// Up to 16, 32 and 64 rows of X.  A wave requests four blocks at a time where there are more than two for each, else fewer
+// (what is requested behind the last block is fetched for nothing).
+hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st) {
+    const int each = (a.kb + SPLIT_WAVES - 1) / SPLIT_WAVES;
+    if (a.T <= 16) {
+        if (each > 2) launch_split<1, 1, 4>(a, st);
+        else launch_split<1, 1, 2>(a, st);
+    } else if (a.T <= 32) {
+        if (each > 2) launch_split<1, 2, 4>(a, st);
+        else launch_split<1, 2, 2>(a, st);
+    } else {
+        launch_split<2, 2, 2>(a, st);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace crisp

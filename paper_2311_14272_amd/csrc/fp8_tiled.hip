@@ -55,21 +55,27 @@ __device__ __forceinline__ void wait_loads() {
 // NS x NT waves, each RS x RT tiles of 32 x 32; STAGES blocks in LDS, all but one of them on their way.  BF16: the result's
 // type, and with it the instruction.  TILES: W has a scale for 128 x 128, one for all of a wave's rows.
 //
+// KG: groups of waves that take the blocks in turn, for sizes whose tiles leave most CUs with one workgroup or none: a step then
+// costs its latencies (a barrier, LDS reads, two dependent matrix instructions: 0.5 us measured), whatever it computes.  Their
+// sums are added up in LDS, in the order of the groups.
+//
 // A step begins when its block has arrived for every wave (each waits for its own share, then all meet) - by then everybody
 // is done with the block before, whose place the next request takes.  All a wave's memory operations are requests to LDS,
 // the same number each step, so that the wait can leave the later steps' ones outstanding.
-template <int NS, int NT, int RS, int RT, int STAGES, bool BF16, bool TILES>
-__global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
+template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
+__global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * NT == 4 ? 1 : 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
     constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
     constexpr int LW = BS / 8 / NW, LX = BT / 8 / NW;            // requests of eight rows that a wave makes per step
     constexpr int LS = ((BS + BT) / 64 + NW - 1) / NW;           // and of 64 scales (some may be nobody's)
     constexpr int SC = LS * NW * 64;
     static_assert(BS % (8 * NW) == 0 && BT % (8 * NW) == 0 && BS % 64 == 0, "whole requests");
     constexpr int PER = LW + LX + LS;
-    __shared__ __align__(16) uint8_t w0[BS * 128], x0[BT * 128], w1[BS * 128], x1[BT * 128];
-    __shared__ __align__(16) uint8_t w2[STAGES > 2 ? BS * 128 : 16], x2[STAGES > 2 ? BT * 128 : 16], w3[STAGES > 3 ? BS * 128 : 16], x3[STAGES > 3 ? BT * 128 : 16];
-    __shared__ __align__(16) float s0_[SC], s1_[SC], s2_[STAGES > 2 ? SC : 4], s3_[STAGES > 3 ? SC : 4];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    constexpr int W = KG * BS * 128, X = KG * BT * 128;
+    __shared__ __align__(16) uint8_t w0[W], x0[X], w1[W], x1[X];
+    __shared__ __align__(16) uint8_t w2[STAGES > 2 ? W : 16], x2[STAGES > 2 ? X : 16], w3[STAGES > 3 ? W : 16], x3[STAGES > 3 ? X : 16];
+    __shared__ __align__(16) float s0_[KG * SC], s1_[KG * SC], s2_[STAGES > 2 ? KG * SC : 4], s3_[STAGES > 3 ? KG * SC : 4];
+    const int lane = threadIdx.x % 64, all = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wave = all % NW, kg = all / NW;                    // (kg is 0 where there is one group)
 
     int id = blockIdx.x;
     const int n = tiles_s * tiles_t, per = n / XCDS;
@@ -113,8 +119,8 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
     int wr[4], xr[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-        wr[c] = (ws * RS * 32 + si) * 128 + ((4 * h + c) ^ w_swizzle(si)) * 16;
-        xr[c] = (wt * RT * 32 + i) * 128 + ((4 * h + c) ^ x_swizzle(i)) * 16;
+        wr[c] = (kg * BS + ws * RS * 32 + si) * 128 + ((4 * h + c) ^ w_swizzle(si)) * 16;
+        xr[c] = (kg * BT + wt * RT * 32 + i) * 128 + ((4 * h + c) ^ x_swizzle(i)) * 16;
     }
 
     f32x16 acc[RS][RT];
@@ -129,13 +135,13 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
     auto request = [&](int n, int b, uint8_t* wl, uint8_t* xl, float* sl) {
         if (n < LS) {
             const int j = n;
-            __builtin_amdgcn_global_load_lds((global_ptr)(sp[j] + b * sstep[j]), (lds_ptr)(sl + (wave + j * NW) * 64), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)(sp[j] + b * sstep[j]), (lds_ptr)(sl + kg * SC + (wave + j * NW) * 64), 4, 0, 0);
         } else if (n < LS + LW) {
             const int j = n - LS;
-            __builtin_amdgcn_global_load_lds((global_ptr)(wb + (int64_t)b * 128 + wo[j]), (lds_ptr)(wl + (wave + j * NW) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)(wb + (int64_t)b * 128 + wo[j]), (lds_ptr)(wl + (kg * (BS / 8) + wave + j * NW) * 1024), 16, 0, 0);
         } else {
             const int j = n - LS - LW;
-            __builtin_amdgcn_global_load_lds((global_ptr)(xb + (int64_t)b * 128 + xo[j]), (lds_ptr)(xl + (wave + j * NW) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)(xb + (int64_t)b * 128 + xo[j]), (lds_ptr)(xl + (kg * (BT / 8) + wave + j * NW) * 1024), 16, 0, 0);
         }
     };
     auto fetch = [&](int b, uint8_t* wl, uint8_t* xl, float* sl) {
@@ -156,8 +162,8 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
 #pragma unroll
             for (int c = 0; c < 4; ++c) xv[q][c] = *reinterpret_cast<const i32x4*>(xl + xr[c] + q * 4096);
 #pragma unroll
-        for (int q = 0; q < RT; ++q) f[q] = sl[BS + (wt * RT + q) * 32 + i];
-        const float wscale = TILES ? sl[ws * RS * 32] : 0.0f;
+        for (int q = 0; q < RT; ++q) f[q] = sl[kg * SC + BS + (wt * RT + q) * 32 + i];
+        const float wscale = TILES ? sl[kg * SC + ws * RS * 32] : 0.0f;
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 xw[BF16 ? 1 : RT][8];
         if constexpr (!BF16) {
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
                 const int r = (k - 1) / RT, q = (k - 1) % RT;
                 if (!TILES && q == 0) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(sl + (ws * RS + r) * 32 + 16 * h + 4 * c);
+                    for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(sl + kg * SC + (ws * RS + r) * 32 + 16 * h + 4 * c);
                 }
 #pragma unroll
                 for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
@@ -222,19 +228,21 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
     // (behind the last block the requests repeat it, into places that nobody reads any more: a step is then free of branches)
 #define CRISP_STEP(k, here, there)                                                                                \
     {                                                                                                             \
-        const int b = b0 + k, ahead = min(b + AHEAD, a.kb - 1);                                                   \
+        const int step = step0 + k, b = step * KG + kg, ahead = min(b + AHEAD * KG, a.kb - 1);                    \
         wait_loads<(AHEAD - 1) * PER>();                                                                          \
         __builtin_amdgcn_s_barrier();                                                                             \
+        if (KG > 1 && b >= a.kb) break;               /* the last step may have no block for the later groups */  \
         compute(w##here, x##here, s##here##_, [&](int tile) {                                                     \
             _Pragma("unroll") for (int n = 0; n < PER; ++n)                                                       \
-                if (n * SPREAD / PER == tile) request(n, ahead, w##there, x##there, s##there##_);                \
+                if (n * SPREAD / PER == tile) request(n, ahead, w##there, x##there, s##there##_);                 \
         });                                                                                                       \
-        if (b + 1 >= a.kb) break;                                                                                 \
+        if (step + 1 >= steps) break;                                                                             \
     }
-    fetch(0, w0, x0, s0_);
-    if constexpr (AHEAD > 1) fetch(min(1, a.kb - 1), w1, x1, s1_);
-    if constexpr (AHEAD > 2) fetch(min(2, a.kb - 1), w2, x2, s2_);
-    for (int b0 = 0;; b0 += STAGES) {
+    const int steps = (a.kb + KG - 1) / KG;
+    fetch(min(kg, a.kb - 1), w0, x0, s0_);
+    if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), w1, x1, s1_);
+    if constexpr (AHEAD > 2) fetch(min(2 * KG + kg, a.kb - 1), w2, x2, s2_);
+    for (int step0 = 0;; step0 += STAGES) {
         if constexpr (STAGES == 2) {
             CRISP_STEP(0, 0, 1) CRISP_STEP(1, 1, 0)
         } else if constexpr (STAGES == 3) {
@@ -245,6 +253,36 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
     }
 #undef CRISP_STEP
     wait_loads<0>();
+    if constexpr (KG > 1) {
+        static_assert(W >= BS * BT * 4, "a group's sums fit one stage's rows of W");
+        f32x16* part = reinterpret_cast<f32x16*>(w0);
+#pragma unroll
+        for (int g = 1; g < KG; ++g) {
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < RS; ++r)
+#pragma unroll
+                for (int q = 0; q < RT; ++q) {
+                    f32x4* p = reinterpret_cast<f32x4*>(part + ((wave * RS + r) * RT + q) * 64);     // four registers of all lanes at a time
+                    if (kg == g) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) p[j * 64 + lane] = f32x4{acc[r][q][4 * j], acc[r][q][4 * j + 1], acc[r][q][4 * j + 2], acc[r][q][4 * j + 3]};
+                    }
+                }
+            __syncthreads();
+            if (kg == 0) {
+#pragma unroll
+                for (int r = 0; r < RS; ++r)
+#pragma unroll
+                    for (int q = 0; q < RT; ++q) {
+                        const f32x4* p = reinterpret_cast<const f32x4*>(part + ((wave * RS + r) * RT + q) * 64);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) acc[r][q][j] += p[j / 4 * 64 + lane][j % 4];
+                    }
+            }
+        }
+        if (kg > 0) return;
+    }
 
     const bool plain = !a.scale && !a.bias && !a.residual && !a.relu && ((uintptr_t)a.y & 15) == 0 && a.ldy % (BF16 ? 8 : 4) == 0;
 #pragma unroll
@@ -254,26 +292,44 @@ __global__ __launch_bounds__(64 * NS * NT, 2) void fp8_tiled_kernel(ProductArgs 
             store_y16<BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, acc[r][q], plain);
 }
 
-template <int NS, int NT, int RS, int RT, int STAGES, bool BF16>
+template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16>
 static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + NS * RS * 32 - 1) / (NS * RS * 32), tt = (a.T + NT * RT * 32 - 1) / (NT * RT * 32);
-    auto kernel = a.w_tiles ? fp8_tiled_kernel<NS, NT, RS, RT, STAGES, BF16, true> : fp8_tiled_kernel<NS, NT, RS, RT, STAGES, BF16, false>;
-    kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT, 0, st>>>(a, ts, tt);
+    auto kernel = a.w_tiles || RS * RT == 8 ? fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, true> : fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, RS * RT == 8>;
+    kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT * KG, 0, st>>>(a, ts, tt);
 }
 
+// The tile: the fewest rounds of 256 workgroups (each takes a CU's LDS) times what a step of a block takes, in microseconds as
+// measured with S = K = 4096 and T = 128 .. 4096.  Results in fp32 have twice the matrix work and the widening, and no registers
+// left for 256 x 256.  W with a scale for each row costs registers too (256 x 256 spills).
+//
+//   T of S = K = 4096, bf16, us:   128    256    512   1024   2048   4096
+//   64 x 64, two groups           13.3   13.5   24.2   48     94
+//   128 x 64, two groups          17.5   17.3   17.8   33.5   65.7
+//   128 x 128                     24.3   24.3   24.4   25.3   49.6
+//   128 x 256                                   32.8   33.4   38.6   70
+//   256 x 256                                                 62     61
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
-    const int64_t big = (int64_t)((a.S + 255) / 256) * ((a.T + 255) / 256);
-    const int64_t mid = (int64_t)((a.S + 127) / 128) * ((a.T + 127) / 128);
-    // 256 x 256 tiles where they fill three quarters of the CUs.  Widening to bf16 takes more registers than such a wave has
-    // left: 128 x 128 for fp32 results (4096 x 4096 x 4096: 660 TFLOP/s with 256 x 256, 980 at half the rows with 128 x 128).
-    if (a.y_bf16) {
-        if (big >= 192 && a.w_tiles) launch_tiles<2, 4, 4, 2, 2, true>(a, st);
-        else if (mid > 256) launch_tiles<2, 2, 2, 2, 2, true>(a, st);
-        else if (mid >= 192) launch_tiles<2, 2, 2, 2, 4, true>(a, st);
-        else launch_tiles<2, 2, 2, 1, 4, true>(a, st);
-    } else {
-        if (mid >= 192) launch_tiles<2, 2, 2, 2, 2, false>(a, st);
-        else launch_tiles<2, 2, 2, 1, 4, false>(a, st);
+    static const struct { int bs, bt; float step[2]; } shapes[] = {         // [BF16]
+        {64, 64, {0.45f, 0.40f}}, {128, 64, {0.65f, 0.53f}}, {128, 128, {1.2f, 0.76f}}, {128, 256, {2.15f, 1.15f}}, {256, 256, {0.0f, 1.9f}}};
+    int best = 0;
+    float least = 0.0f;
+    for (int k = 0; k < 5; ++k) {
+        if (k == 4 && !(a.y_bf16 && a.w_tiles)) continue;
+        const int64_t n = (int64_t)((a.S + shapes[k].bs - 1) / shapes[k].bs) * ((a.T + shapes[k].bt - 1) / shapes[k].bt);
+        const float cost = (float)((n + 255) / 256) * shapes[k].step[a.y_bf16];
+        if (k == 0 || cost < least) { best = k; least = cost; }
+    }
+    switch (best * 2 + a.y_bf16) {
+        case 0: launch_tiles<2, 2, 1, 1, 3, 2, false>(a, st); break;
+        case 1: launch_tiles<2, 2, 1, 1, 3, 2, true>(a, st); break;
+        case 2: launch_tiles<2, 2, 2, 1, 3, 2, false>(a, st); break;
+        case 3: launch_tiles<2, 2, 2, 1, 3, 2, true>(a, st); break;
+        case 4: launch_tiles<2, 4, 2, 1, 4, 1, false>(a, st); break;
+        case 5: launch_tiles<2, 4, 2, 1, 4, 1, true>(a, st); break;
+        case 6: launch_tiles<2, 4, 2, 2, 3, 1, false>(a, st); break;
+        case 7: launch_tiles<2, 4, 2, 2, 3, 1, true>(a, st); break;
+        default: launch_tiles<2, 4, 4, 2, 2, 1, true>(a, st); break;
     }
     return hipGetLastError();
 }

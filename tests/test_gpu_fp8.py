@@ -126,7 +126,8 @@ def _pair(seed, T, S, K, w_tiles):
 PRODUCTS = [(1, 1, 1), (1, 16, 128), (2, 48, 100), (1, 1000, 4096), (5, 130, 640), (16, 128, 1152), (17, 33, 257), (31, 520, 2050),
             (48, 64, 8192), (64, 4096, 256), (65, 200, 384), (100, 129, 1000), (128, 128, 128), (129, 300, 512), (255, 257, 300),
             (256, 256, 256), (333, 1000, 130), (512, 512, 1152), (700, 384, 2304), (1030, 1025, 140),
-            (3400, 3841, 260), (4096, 4096, 128)]
+            (3400, 3841, 260), (4096, 4096, 128), (20, 60, 9000), (1000, 40, 300), (90, 70, 200), (1100, 2000, 384),
+            (2100, 2050, 200), (65, 65, 65), (80, 96, 1000)]
 
 
 @pytest.mark.parametrize("w_tiles", [True, False], ids=["tiles", "rows"])
@@ -225,6 +226,21 @@ def test_linear_is_quantize_and_product(shape, dtype):
             assert torch.equal(fp8.linear(x, weights), fp8.product(x8, weights))
             assert torch.equal(fp8.linear(x, weights, out_dtype=torch.float32, bias=bias),
                                fp8.product(x8, weights, out_dtype=torch.float32, bias=bias))
+
+
+def test_rows_far_apart_in_many():
+    """Row strides of 2^24 and more: more rows than the kernels without staging are chosen for by their number."""
+    ld, K = 1 << 24, 200
+    q = torch.zeros((70, ld), dtype=torch.uint8, device="cuda")
+    x, w = torch.randn((70, K), device="cuda"), torch.randn((90, K), device="cuda")
+    far = fp8.Fp8Mat(q, torch.zeros((2, 70), device="cuda"), 70, K, fp8.ROWS)
+    fp8.quantize(x, out=far)
+    x8 = fp8.quantize(x)
+    for kind in (fp8.TILES, fp8.ROWS):
+        w8 = fp8.quantize(w, kind)
+        A = np.abs(U.held(_np(x8.q), _np(x8.scale), False)) @ np.abs(U.held(_np(w8.q), _np(w8.scale), kind == fp8.TILES)).T
+        a, b = (_np(fp8.product(m, w8, out_dtype=torch.float32)).astype(np.float64) for m in (far, x8))
+        assert (np.abs(a - b) <= 2 * U.product_bound(A, K)).all()
 
 
 def test_long_offsets():
