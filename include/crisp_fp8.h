@@ -79,12 +79,13 @@ CRISP_API crisp_status crisp_fp8_quant(const void *X, int32_t in_type, int64_t r
 CRISP_API crisp_status crisp_fp8_product(const crisp_fp8_mat *X, const crisp_fp8_mat *W, void *Y, int64_t ldy,
                                          int32_t y_type, const crisp_epilogue *ep, void *stream);
 
-/* Bytes of workspace that crisp_fp8_linear wants for T rows of K columns (host only; 0 for sizes out of range). */
+/* Bytes of workspace that crisp_fp8_linear wants for T rows of K columns (host only; 0 for a few rows, and for sizes out of
+ * range). */
 CRISP_API size_t crisp_fp8_linear_ws(int64_t T, int64_t K);
 
 /*
  * The layer from activations that are not in 8 bits yet: crisp_fp8_quant (ROWS) of X into ws, then crisp_fp8_product; for a
- * few rows one kernel does both and ws is not touched.  Results are those of the two calls, bit for bit.
+ * few rows one kernel does both and ws is not looked at.  Results are those of the two calls, bit for bit.
  *   X: T x ldx, fp32 or bf16 per in_type (device), aligned to its element; ldx >= W->cols.
  *   ws: crisp_fp8_linear_ws(T, W->cols) bytes (device), 16-byte aligned; its contents are unspecified before and after.
  *      Calls that may run at the same time need one each.
@@ -93,6 +94,24 @@ CRISP_API size_t crisp_fp8_linear_ws(int64_t T, int64_t K);
 CRISP_API crisp_status crisp_fp8_linear(const void *X, int32_t in_type, int64_t T, int64_t ldx, const crisp_fp8_mat *W,
                                         void *Y, int64_t ldy, int32_t y_type, const crisp_epilogue *ep, void *ws,
                                         size_t ws_bytes, void *stream);
+
+/* Bytes of workspace of crisp_fp8_linear_backward (host only; 0 for sizes out of range). */
+CRISP_API size_t crisp_fp8_linear_backward_ws(int64_t T, int64_t S);
+
+/*
+ * The layer's gradients: dY is quantised once, along its rows and along its columns, then
+ *   dX = crisp_fp8_product(dY, Wt)     (T x K, lddx >= K, fp32 or bf16 per dx_type),
+ *   dW = crisp_fp8_product(dY^T, Xt)   (S x K, lddw >= K, fp32 or bf16 per dw_type), with accumulate = 1 added to what is there.
+ *   dY: T x ldg of S used columns, fp32 or bf16 per in_type (device), aligned to its element.
+ *   Xt: the activations' transpose (K x T, ROWS or TILES);  Wt: the weights' transpose (K x S).
+ *   dX or dW may be NULL: that gradient is not computed, and Wt or Xt is not looked at.
+ *   ws: crisp_fp8_linear_backward_ws(T, S) bytes (device), 16-byte aligned; as in crisp_fp8_linear.
+ * Errors: EINVAL, ESHAPE, EALIGN, EBUFSIZE, EDEVICE.
+ */
+CRISP_API crisp_status crisp_fp8_linear_backward(const void *dY, int32_t in_type, int64_t T, int64_t S, int64_t ldg,
+                                                 const crisp_fp8_mat *Xt, const crisp_fp8_mat *Wt, void *dX, int64_t lddx,
+                                                 int32_t dx_type, void *dW, int64_t lddw, int32_t dw_type, int32_t accumulate,
+                                                 void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -118,7 +118,7 @@ def set_live(out, lr, step, grad_scale=1.0, skip=False):
 
 def step(batch: Batch, lr=0.0, beta1=0.9, beta2=0.999, eps=1e-8, step=1, grad_scale=1.0, live=None):
     """crisp_adamw_batch: one step of all tensors, in place.  live: see live(); lr, step and grad_scale are then its."""
-    if batch.device.index != torch.cuda.current_device():
+    if batch.device.index != torch._C._cuda_getDevice():
         raise ValueError("the tensors are on %s, not on the current GPU" % batch.device)
     if live is not None and (live.dtype != torch.int32 or live.numel() != 4 or not live.is_contiguous()):
         raise ValueError("live: four int32 words, as live() makes them")

@@ -79,9 +79,17 @@ crisp_status crisp_fp8_product(const crisp_fp8_mat* X, const crisp_fp8_mat* W, v
 }
 
 size_t crisp_fp8_linear_ws(int64_t T, int64_t K) {
-    if (T < 1 || K < 1 || T > MOST || K > MOST || too_many(T, K)) return 0;
+    if (T < 1 || K < 1 || T > MOST || K > MOST || too_many(T, K) || fp8_takes_raw(T, K)) return 0;
     return (size_t)T * blocks(K) * (FP8_BLOCK + sizeof(float));
 }
+
+// A matrix in ROWS inside a workspace, codes first.
+static crisp_fp8_mat mat_in(void* ws, int64_t rows, int64_t cols) {
+    const int64_t ld = blocks(cols) * FP8_BLOCK;
+    uint8_t* q = static_cast<uint8_t*>(ws);
+    return crisp_fp8_mat{q, reinterpret_cast<float*>(q + rows * ld), ld, rows, rows, cols, CRISP_FP8_ROWS, 0};
+}
+static size_t mat_bytes(int64_t rows, int64_t cols) { return ((size_t)rows * blocks(cols) * (FP8_BLOCK + sizeof(float)) + 15) / 16 * 16; }
 
 crisp_status crisp_fp8_linear(const void* X, int32_t in_type, int64_t T, int64_t ldx, const crisp_fp8_mat* W, void* Y, int64_t ldy,
                               int32_t y_type, const crisp_epilogue* ep, void* ws, size_t ws_bytes, void* stream) {
@@ -89,13 +97,51 @@ crisp_status crisp_fp8_linear(const void* X, int32_t in_type, int64_t T, int64_t
     crisp_status st = check_mat(W);
     if (st != CRISP_OK || (st = check_in(X, in_type, T, W->cols, ldx)) != CRISP_OK) return st;
     if ((st = check_out(Y, T, W->rows, W->ld, ldy, y_type, ep)) != CRISP_OK) return st;
+    hipError_t e;
+    if (fp8_takes_raw(T, W->cols)) {
+        e = launch_fp8_raw(X, in_type, T, ldx, *W, Y, ldy, y_type, ep, (hipStream_t)stream);
+    } else {
+        if (off(ws, 16)) return CRISP_EALIGN;
+        if (!ws || ws_bytes < crisp_fp8_linear_ws(T, W->cols)) return CRISP_EBUFSIZE;
+        const crisp_fp8_mat q = mat_in(ws, T, W->cols);
+        e = launch_fp8_quant(X, in_type, T, W->cols, ldx, nullptr, &q, nullptr, (hipStream_t)stream);
+        if (e == hipSuccess) e = launch_fp8_product(q, *W, Y, ldy, y_type, ep, (hipStream_t)stream);
+    }
+    return e == hipSuccess ? CRISP_OK : CRISP_EDEVICE;
+}
+
+size_t crisp_fp8_linear_backward_ws(int64_t T, int64_t S) {
+    if (T < 1 || S < 1 || T > MOST || S > MOST || too_many(T, S) || too_many(S, T)) return 0;
+    return mat_bytes(T, S) + mat_bytes(S, T);
+}
+
+crisp_status crisp_fp8_linear_backward(const void* dY, int32_t in_type, int64_t T, int64_t S, int64_t ldg, const crisp_fp8_mat* Xt,
+                                       const crisp_fp8_mat* Wt, void* dX, int64_t lddx, int32_t dx_type, void* dW, int64_t lddw,
+                                       int32_t dw_type, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+    if (!dX && !dW) return CRISP_EINVAL;
+    if ((dX && !Wt) || (dW && !Xt) || (accumulate != 0 && accumulate != 1)) return CRISP_EINVAL;
+    crisp_status st = check_in(dY, in_type, T, S, ldg);
+    if (st != CRISP_OK) return st;
+    if (too_many(S, T)) return CRISP_ESHAPE;
+    crisp_epilogue add = {};
+    add.residual = dW; add.ldr = lddw;
+    const crisp_epilogue* ep = accumulate ? &add : nullptr;
+    if (dX) {
+        if ((st = check_mat(Wt)) != CRISP_OK) return st;
+        if (Wt->cols != S) return CRISP_ESHAPE;
+        if ((st = check_out(dX, T, Wt->rows, Wt->ld, lddx, dx_type, nullptr)) != CRISP_OK) return st;
+    }
+    if (dW) {
+        if ((st = check_mat(Xt)) != CRISP_OK) return st;
+        if (Xt->cols != T || (dX && Xt->rows != Wt->rows)) return CRISP_ESHAPE;
+        if ((st = check_out(dW, S, Xt->rows, Xt->ld, lddw, dw_type, ep)) != CRISP_OK) return st;
+    }
     if (off(ws, 16)) return CRISP_EALIGN;
-    if (!ws || ws_bytes < crisp_fp8_linear_ws(T, W->cols)) return CRISP_EBUFSIZE;
-    const int64_t ld = blocks(W->cols) * FP8_BLOCK;
-    const crisp_fp8_mat q = {static_cast<uint8_t*>(ws), reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + T * ld), ld, T, T, W->cols,
-                             CRISP_FP8_ROWS, 0};
-    hipError_t e = launch_fp8_quant(X, in_type, T, W->cols, ldx, nullptr, &q, nullptr, (hipStream_t)stream);
-    if (e == hipSuccess) e = launch_fp8_product(q, *W, Y, ldy, y_type, ep, (hipStream_t)stream);
+    if (!ws || ws_bytes < crisp_fp8_linear_backward_ws(T, S)) return CRISP_EBUFSIZE;
+    const crisp_fp8_mat g = mat_in(ws, T, S), gt = mat_in(static_cast<uint8_t*>(ws) + mat_bytes(T, S), S, T);
+    hipError_t e = launch_fp8_quant(dY, in_type, T, S, ldg, nullptr, dX ? &g : nullptr, dW ? &gt : nullptr, (hipStream_t)stream);
+    if (e == hipSuccess && dX) e = launch_fp8_product(g, *Wt, dX, lddx, dx_type, nullptr, (hipStream_t)stream);
+    if (e == hipSuccess && dW) e = launch_fp8_product(gt, *Xt, dW, lddw, dw_type, ep, (hipStream_t)stream);
     return e == hipSuccess ? CRISP_OK : CRISP_EDEVICE;
 }
 

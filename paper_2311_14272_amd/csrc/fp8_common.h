@@ -64,4 +64,41 @@ __device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
 }
 __device__ __forceinline__ uint16_t to_bf16(float a) { return __builtin_bit_cast(uint16_t, (__bf16)a); }
 
+// Eight elements of a row from column c on; what lies at or behind `cols` counts as zero.  vec: the address is a multiple of
+// 16 bytes wherever c is a multiple of 8.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void* X, int64_t at, int64_t left, bool vec, float (&x)[8]) {
+    if (vec && left >= 8) {
+        if constexpr (BF16) {
+            from_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + at), x);
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
+            const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        x[j] = 0.0f;
+        if (j < left) {
+            if constexpr (BF16) x[j] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(X)[at + j] << 16);
+            else x[j] = static_cast<const float*>(X)[at + j];
+        }
+    }
+}
+
+// 16 lanes' block of 128 elements, eight each: its codes and its scale.
+__device__ __forceinline__ uint2 quantize_block(float (&x)[8], float& scale) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = umax(top, abs_bits(x[j]));
+    scale = fp8_scale(__uint_as_float(max16(top)));
+    const float inv = 1.0f / scale;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= inv;
+    return to_fp8x8(x);
+}
+
 }  // namespace crisp

@@ -24,7 +24,14 @@ struct ProductArgs {
     const float *scale, *bias;
     const void* residual;
     int relu, y_bf16;
+    const void* raw;                    // X before it is quantised (T x K of row stride ldraw), where the kernel does that; else NULL
+    int64_t ldraw;
+    int raw_bf16, raw_vec, K;
 };
+
+// Blocks of X that a workgroup of fp8_split_kernel quantises for itself.  Its 512 threads take 32 of them in 0.2 us; a launch of
+// the quantiser's own costs 2 us more on the GPU and 2 on the host.
+constexpr int FP8_OWN_BLOCKS = 128;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;

@@ -3,20 +3,35 @@
 
 namespace crisp {
 
-hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
-                              const crisp_epilogue* ep, hipStream_t st) {
+static ProductArgs args_of(const crisp_fp8_mat& W, int64_t T, void* Y, int64_t ldy, int y_type, const crisp_epilogue* ep) {
     ProductArgs a = {};
-    a.x = X.q; a.w = W.q; a.xs = X.scale; a.ws = W.scale;
-    a.ldx = X.ld; a.ldw = W.ld; a.ldxs = X.lds; a.ldws = W.lds;
-    a.T = (int)X.rows; a.S = (int)W.rows; a.kb = (int)((X.cols + FP8_BLOCK - 1) / FP8_BLOCK);
+    a.w = W.q; a.ws = W.scale; a.ldw = W.ld; a.ldws = W.lds;
+    a.T = (int)T; a.S = (int)W.rows; a.K = (int)W.cols; a.kb = (int)((W.cols + FP8_BLOCK - 1) / FP8_BLOCK);
     a.w_tiles = W.kind == CRISP_FP8_TILES;
     a.y = Y; a.ldy = ldy; a.y_bf16 = y_type == CRISP_Y_BF16;
     if (ep) { a.scale = ep->scale; a.bias = ep->bias; a.residual = ep->residual; a.ldr = ep->ldr; a.relu = ep->relu; }
+    return a;
+}
+
+hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
+                              const crisp_epilogue* ep, hipStream_t st) {
+    ProductArgs a = args_of(W, X.rows, Y, ldy, y_type, ep);
+    a.x = X.q; a.xs = X.scale; a.ldx = X.ld; a.ldxs = X.lds;
     // Up to 64 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us: 16 rows 6.5
     // against 12 with 64 x 64 tiles, 32: 9.2 and 12.3, 64: 11.7 and 13.5, 128: 18.9 and 13.3).  So is a W of few rows: X is then
     // what is read.  The tiled kernels' offsets inside a tile are 32 bits.
     if (fp8_takes_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw)) return launch_fp8_split(a, st);
     return launch_fp8_tiled(a, st);
+}
+
+bool fp8_takes_raw(int64_t T, int64_t K) { return T <= 16 && T * ((K + FP8_BLOCK - 1) / FP8_BLOCK) <= FP8_OWN_BLOCKS; }
+
+hipError_t launch_fp8_raw(const void* X, int in_type, int64_t T, int64_t ldx, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
+                          const crisp_epilogue* ep, hipStream_t st) {
+    ProductArgs a = args_of(W, T, Y, ldy, y_type, ep);
+    a.raw = X; a.ldraw = ldx; a.raw_bf16 = in_type == CRISP_IN_BF16;
+    a.raw_vec = fp8_whole_vectors(X, in_type, ldx);
+    return launch_fp8_split(a, st);
 }
 
 }  // namespace crisp

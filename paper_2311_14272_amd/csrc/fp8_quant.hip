@@ -5,31 +5,6 @@
 
 namespace crisp {
 
-// Eight elements of a row from column c on; what lies at or behind `cols` counts as zero.  vec: the address is a multiple of
-// 16 bytes wherever c is a multiple of 8.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* X, int64_t at, int64_t left, bool vec, float (&x)[8]) {
-    if (vec && left >= 8) {
-        if constexpr (BF16) {
-            from_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + at), x);
-        } else {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
-            const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at + 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[j] = 0.0f;
-        if (j < left) {
-            if constexpr (BF16) x[j] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(X)[at + j] << 16);
-            else x[j] = static_cast<const float*>(X)[at + j];
-        }
-    }
-}
-
 // ROWS, one direction, no mask: 16 lanes take a block of 128 columns, a workgroup 16 consecutive blocks of the matrix in
 // row order.
 template <bool BF16>
@@ -41,15 +16,9 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const void* __restrict__ 
     const int b = (int)(id - r * kb), lane = threadIdx.x % 16;
     if (r >= rows) return;      // all 16 lanes of a group leave together
     const int c = b * FP8_BLOCK + lane * 8;
-    float x[8];
+    float x[8], s;
     load8<BF16>(X, r * ldx + c, cols - c, vec, x);
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = umax(top, abs_bits(x[j]));
-    const float s = fp8_scale(__uint_as_float(max16(top))), inv = 1.0f / s;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] *= inv;
-    *reinterpret_cast<uint2*>(q + r * ld + c) = to_fp8x8(x);
+    *reinterpret_cast<uint2*>(q + r * ld + c) = quantize_block(x, s);
     if (lane == 0) scale[b * lds + r] = s;
 }
 
@@ -170,7 +139,7 @@ __global__ __launch_bounds__(256) void fp8_tile_kernel(const void* __restrict__ 
 hipError_t launch_fp8_quant(const void* X, int in_type, int64_t rows, int64_t cols, int64_t ldx, const uint32_t* mask,
                             const crisp_fp8_mat* Q, const crisp_fp8_mat* Qt, hipStream_t st) {
     const bool bf16 = in_type == CRISP_IN_BF16;
-    const bool vec = ((uintptr_t)X & 15) == 0 && (ldx * (bf16 ? 2 : 4)) % 16 == 0;
+    const bool vec = fp8_whole_vectors(X, in_type, ldx);
     const int64_t rb = (rows + FP8_BLOCK - 1) / FP8_BLOCK, cb = (cols + FP8_BLOCK - 1) / FP8_BLOCK;
     const int kind = Q ? Q->kind : Qt->kind;
     if (kind == CRISP_FP8_ROWS && !Qt && !mask) {

@@ -26,16 +26,19 @@ __device__ __forceinline__ f32x4 block_sum(const i32x4 (&w)[2], const i32x4 (&x)
     }
 }
 
-// U: blocks that a wave requests at a time.
-template <int MS, int MT, int U, bool BF16, bool TILES>
+// U: blocks that a wave requests at a time.  RAW: X is not in 8 bits yet; the workgroup quantises it into LDS, all of it, while its
+// first weights are on their way (16 rows at most, and FP8_OWN_BLOCKS blocks).
+template <int MS, int MT, int U, bool BF16, bool TILES, bool RAW>
 __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs a, int tiles_s) {
     __shared__ f32x4 part[SPLIT_WAVES][MS * MT][64];
+    __shared__ __align__(16) uint8_t own_q[RAW ? FP8_OWN_BLOCKS * 128 : 16];
+    __shared__ float own_s[RAW ? FP8_OWN_BLOCKS : 1];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int i = lane % 16, h = lane / 16;
     const int s0 = (int)(blockIdx.x % tiles_s) * (16 * MS), t0 = (int)(blockIdx.x / tiles_s) * (16 * MT);
     // rows behind the last one repeat it, their results are not stored
-    const uint8_t *w[MS], *x[MT];
-    const float* xs[MT];
+    const uint8_t *w[MS], *x[MT] = {};
+    const float* xs[MT] = {};
     const float* wsp[MS];
 #pragma unroll
     for (int r = 0; r < MS; ++r) {
@@ -43,7 +46,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
         wsp[r] = TILES ? a.ws + min(s0 + 16 * r, a.S - 1) / 128 * a.ldws : a.ws;
     }
 #pragma unroll
-    for (int q = 0; q < MT; ++q) {
+    for (int q = 0; q < (RAW ? 0 : MT); ++q) {
         const int t = min(t0 + 16 * q + i, a.T - 1);
         x[q] = a.x + t * a.ldx + h * 32;
         xs[q] = a.xs + t;
@@ -54,9 +57,9 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
 #pragma unroll
         for (int q = 0; q < MT; ++q) sum[r][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    for (int b0 = wave; b0 < a.kb; b0 += U * SPLIT_WAVES) {
-        i32x4 wv[U][MS][2], xv[U][MT][2];
-        float f[U][MT], g[U][MS][TILES ? 1 : 4];
+    i32x4 wv[U][MS][2];
+    float g[U][MS][TILES ? 1 : 4];
+    auto weights = [&](int b0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int b = min(b0 + u * SPLIT_WAVES, a.kb - 1);       // (behind the last block it is fetched again and left out)
@@ -71,11 +74,46 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
                     for (int j = 0; j < 4; ++j) g[u][r][j] = a.ws[b * a.ldws + min(s0 + 16 * r + 4 * h + j, a.S - 1)];
                 }
             }
+        }
+    };
+    if constexpr (RAW) {
+        static_assert(MT == 1, "one tile of X rows");
+        weights(wave);
+        __builtin_amdgcn_sched_barrier(0);
+        const int blocks = a.T * a.kb;
+        for (int e0 = 0; e0 < blocks; e0 += 4 * SPLIT_WAVES) {
+            const int e = e0 + threadIdx.x / 16;
+            if (e < blocks) {
+                const int t = e / a.kb, c = (e - t * a.kb) * 128 + threadIdx.x % 16 * 8;
+                float v[8], scale;
+                if (a.raw_bf16) load8<true>(a.raw, t * a.ldraw + c, a.K - c, a.raw_vec, v);
+                else load8<false>(a.raw, t * a.ldraw + c, a.K - c, a.raw_vec, v);
+                *reinterpret_cast<uint2*>(own_q + e * 128 + threadIdx.x % 16 * 8) = quantize_block(v, scale);
+                if (threadIdx.x % 16 == 0) own_s[e] = scale;
+            }
+        }
+        __syncthreads();
+    }
+
+    for (int b0 = wave; b0 < a.kb; b0 += U * SPLIT_WAVES) {
+        i32x4 xv[U][MT][2];
+        float f[U][MT];
+        if (!RAW || b0 != wave) weights(b0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int b = min(b0 + u * SPLIT_WAVES, a.kb - 1);
 #pragma unroll
             for (int q = 0; q < MT; ++q) {
-                xv[u][q][0] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128);
-                xv[u][q][1] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128 + 16);
-                f[u][q] = xs[q][b * a.ldxs];
+                if constexpr (RAW) {
+                    const int e = min(i, a.T - 1) * a.kb + b;
+                    xv[u][q][0] = *reinterpret_cast<const i32x4*>(own_q + e * 128 + h * 32);
+                    xv[u][q][1] = *reinterpret_cast<const i32x4*>(own_q + e * 128 + h * 32 + 16);
+                    f[u][q] = own_s[e];
+                } else {
+                    xv[u][q][0] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128);
+                    xv[u][q][1] = *reinterpret_cast<const i32x4*>(x[q] + (int64_t)b * 128 + 16);
+                    f[u][q] = xs[q][b * a.ldxs];
+                }
             }
         }
         __builtin_amdgcn_sched_barrier(0);       // all requests first
@@ -115,11 +153,11 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
     }
 }
 
-template <int MS, int MT, int U>
+template <int MS, int MT, int U, bool RAW = false>
 static void launch_split(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + 16 * MS - 1) / (16 * MS), tt = (a.T + 16 * MT - 1) / (16 * MT);
-    auto kernel = a.y_bf16 ? (a.w_tiles ? fp8_split_kernel<MS, MT, U, true, true> : fp8_split_kernel<MS, MT, U, true, false>)
-                           : (a.w_tiles ? fp8_split_kernel<MS, MT, U, false, true> : fp8_split_kernel<MS, MT, U, false, false>);
+    auto kernel = a.y_bf16 ? (a.w_tiles ? fp8_split_kernel<MS, MT, U, true, true, RAW> : fp8_split_kernel<MS, MT, U, true, false, RAW>)
+                           : (a.w_tiles ? fp8_split_kernel<MS, MT, U, false, true, RAW> : fp8_split_kernel<MS, MT, U, false, false, RAW>);
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * SPLIT_WAVES, 0, st>>>(a, ts);
 }
 
@@ -127,7 +165,10 @@ static void launch_split(const ProductArgs& a, hipStream_t st) {
 // (what is requested behind the last block is fetched for nothing).
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st) {
     const int each = (a.kb + SPLIT_WAVES - 1) / SPLIT_WAVES;
-    if (a.T <= 16) {
+    if (a.raw) {
+        if (each > 2) launch_split<1, 1, 4, true>(a, st);
+        else launch_split<1, 1, 2, true>(a, st);
+    } else if (a.T <= 16) {
         if (each > 2) launch_split<1, 1, 4>(a, st);
         else launch_split<1, 1, 2>(a, st);
     } else if (a.T <= 32) {

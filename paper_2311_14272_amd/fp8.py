@@ -40,17 +40,18 @@ def lib():
         L.crisp_fp8_quant.argtypes = [vp, i32, i64, i64, i64, vp, mat, mat, vp]
         L.crisp_fp8_product.argtypes = [mat, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp]
         L.crisp_fp8_linear.argtypes = [vp, i32, i64, i64, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp, C.c_size_t, vp]
-        L.crisp_fp8_linear_ws.argtypes = [i64, i64]
-        for f in (L.crisp_fp8_quant, L.crisp_fp8_product, L.crisp_fp8_linear):
+        L.crisp_fp8_linear_backward.argtypes = [vp, i32, i64, i64, i64, mat, mat, vp, i64, i32, vp, i64, i32, i32, vp, C.c_size_t, vp]
+        for f in (L.crisp_fp8_quant, L.crisp_fp8_product, L.crisp_fp8_linear, L.crisp_fp8_linear_backward):
             f.restype = i32
-        L.crisp_fp8_linear_ws.restype = C.c_size_t
+        for f in (L.crisp_fp8_linear_ws, L.crisp_fp8_linear_backward_ws):
+            f.argtypes, f.restype = [i64, i64], C.c_size_t
         _lib = L
     return _lib
 
 
 def _here(t, what):
     """A tensor's address; it has to be on the device whose stream the work goes to."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
         raise ValueError("%s is on %s, not on the current GPU" % (what, t.device))
     return t.data_ptr()
 
@@ -73,6 +74,10 @@ class Fp8Mat:
             raise ValueError("q: %d rows of at least %d bytes, each row contiguous" % (rows, _blocks(cols) * BLOCK))
         if scale.dtype != torch.float32 or scale.dim() != 2 or tuple(scale.shape) != want or (scale.stride(1) != 1 and want[1] > 1):
             raise ValueError("scale: %d x %d fp32, each row contiguous" % want)
+        self._fill(q, scale, rows, cols, kind)
+
+    def _fill(self, q, scale, rows, cols, kind):
+        want = scale.shape
         self.q, self.scale, self.rows, self.cols, self.kind = q, scale, rows, cols, kind
         # (a tensor of one row may carry any row stride)
         self.c = _Mat(_here(q, "q"), _here(scale, "scale"), q.stride(0) if rows > 1 else max(q.stride(0), q.shape[1]),
@@ -81,9 +86,13 @@ class Fp8Mat:
 
 def alloc_mat(rows, cols, kind=ROWS, device="cuda") -> Fp8Mat:
     """Buffers of a rows x cols matrix in 8 bits, to be filled by quantize."""
-    q = torch.empty((rows, _blocks(cols) * BLOCK), dtype=torch.float8_e4m3fn, device=device)
-    shape = (_blocks(cols), rows) if kind == ROWS else (_blocks(rows), _blocks(cols))
-    return Fp8Mat(q, torch.empty(shape, dtype=torch.float32, device=device), rows, cols, kind)
+    if kind not in (ROWS, TILES) or rows < 1 or cols < 1:
+        raise ValueError("a matrix of at least 1 x 1, kind ROWS or TILES")
+    b = _blocks(cols)
+    q = torch.empty((rows, b * BLOCK), dtype=torch.float8_e4m3fn, device=device)
+    out = Fp8Mat.__new__(Fp8Mat)
+    out._fill(q, torch.empty((b, rows) if kind == ROWS else (_blocks(rows), b), dtype=torch.float32, device=device), rows, cols, kind)
+    return out
 
 
 def _input(x):
@@ -163,25 +172,40 @@ def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None,
         raise ValueError("x has %d columns, the weights %d" % (K, w.cols))
     out = _output(T, w.rows, out, out_dtype, x.device)
     ep = _epilogue(ep, bias, w.rows)
+    L = lib()
     if ws is None:
-        ws = torch.empty(max(16, lib().crisp_fp8_linear_ws(T, K)), dtype=torch.uint8, device=x.device)
-    st = lib().crisp_fp8_linear(p, kind, T, ldx, C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
-                                C.byref(ep) if ep is not None else None, _here(ws, "ws"), ws.numel() * ws.element_size(),
-                                crisp._stream())
+        need = L.crisp_fp8_linear_ws(T, K)
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    st = L.crisp_fp8_linear(p, kind, T, ldx, C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
+                            C.byref(ep) if ep is not None else None, None if ws is None else _here(ws, "ws"),
+                            0 if ws is None else ws.numel() * ws.element_size(), crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_linear", st)
     return out
 
 
-def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=False):
-    """Gradients of y = linear(x, w): (dx, dw) from dy (T x S, fp32 or bf16), x_t = x^T in 8 bits (K x T) and w_t = W^T in 8
-    bits (K x S).  dx is T x K, bf16 unless given; dw is S x K, fp32 unless given.  accumulate: dw (given) += the gradient."""
-    T, S = dy.shape
-    if x_t.cols != T or w_t.cols != S or x_t.rows != w_t.rows:
-        raise ValueError("dy is %d x %d, x^T %d x %d, W^T %d x %d" % (T, S, x_t.rows, x_t.cols, w_t.rows, w_t.cols))
-    if accumulate and dw is None:
-        raise ValueError("accumulate adds to a dw that is given")
-    dy8, dy_t = quantize_both(dy)
-    dx = product(dy8, w_t, dx)
-    ep = crisp.epilogue(residual=dw, ldr=_ld(dw)) if accumulate else None
-    return dx, product(dy_t, x_t, dw, torch.float32, ep=ep)
+def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=False, ws=None):
+    """crisp_fp8_linear_backward, the gradients of y = linear(x, w): (dx, dw) from dy (T x S, fp32 or bf16), x_t = x^T in 8 bits
+    (K x T) and w_t = W^T in 8 bits (K x S); x_t or w_t None: that gradient (dw or dx) is not computed.  dx is T x K, bf16 unless
+    given; dw is S x K, fp32 unless given.  accumulate: dw (given) += the gradient.  ws: as in linear
+    (crisp_fp8_linear_backward_ws bytes)."""
+    p, kind, T, S, ldg = _input(dy)
+    if (x_t is not None and x_t.cols != T) or (w_t is not None and w_t.cols != S):
+        raise ValueError("dy is %d x %d, x^T has %s columns, W^T %s" % (T, S, x_t and x_t.cols, w_t and w_t.cols))
+    if (accumulate and dw is None) or (dx is not None and w_t is None) or (dw is not None and x_t is None):
+        raise ValueError("accumulate adds to a dw that is given; dx needs w_t, dw needs x_t")
+    L = lib()
+    if w_t is not None:
+        dx = _output(T, w_t.rows, dx, torch.bfloat16, dy.device)
+    if x_t is not None:
+        dw = _output(S, x_t.rows, dw, torch.float32, dy.device)
+    if ws is None:
+        ws = torch.empty(max(16, L.crisp_fp8_linear_backward_ws(T, S)), dtype=torch.uint8, device=dy.device)
+    none = (None, 0, 0)
+    st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, None if x_t is None else C.byref(x_t.c), None if w_t is None else C.byref(w_t.c),
+                                     *(none if dx is None else (_here(dx, "dx"), _ld(dx), _IN[dx.dtype])),
+                                     *(none if dw is None else (_here(dw, "dw"), _ld(dw), _IN[dw.dtype])), int(accumulate),
+                                     _here(ws, "ws"), ws.numel() * ws.element_size(), crisp._stream())
+    if st != crisp.OK:
+        raise crisp.CrispError("crisp_fp8_linear_backward", st)
+    return dx, dw

@@ -209,7 +209,8 @@ def test_product_keeps_rows_apart():
     assert y[bad].isnan().all() and torch.equal(y[~bad], clean[~bad])
 
 
-@pytest.mark.parametrize("shape", [(1, 1, 5), (1, 300, 4096), (2, 64, 256), (4, 513, 1100), (7, 96, 384), (8, 256, 8192), (13, 700, 2050),
+@pytest.mark.parametrize("shape", [(1, 1, 5), (1, 300, 4096), (2, 64, 256), (4, 513, 1100), (7, 96, 384), (8, 256, 8192), (1, 33, 16384), (1, 50, 16385), (2, 200, 8000), (16, 40, 1024),
+                                   (15, 512, 1000), (17, 64, 128), (13, 700, 2050),
                                    (16, 128, 128), (33, 200, 1152), (300, 264, 640)], ids=str)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 def test_linear_is_quantize_and_product(shape, dtype):
@@ -297,6 +298,11 @@ def test_backward(shape):
         size = np.abs(d) @ np.abs(wv).T if at == 0 else np.abs(dt) @ np.abs(xv).T
         slack = (U.product_bound(size, T if at else S) * np.abs(direction)).sum() + 1e-10 * (abs(hi) + abs(lo))
         assert abs((hi - lo) / 2 - float((_np(got).astype(np.float64) * direction).sum())) <= slack
+    # one gradient alone, and the two calls it is made of
+    assert torch.equal(fp8.linear_backward(dy, None, w_t, dx=torch.empty((T, K), device="cuda"))[0], dx32)
+    none, alone = fp8.linear_backward(dy, x_t, None)
+    dy8, dy_t = fp8.quantize_both(dy)
+    assert none is None and torch.equal(alone, dw) and torch.equal(fp8.product(dy_t, x_t, out_dtype=torch.float32), dw)
     again, acc = fp8.linear_backward(dy, x_t, w_t, dw=dw.clone(), accumulate=True)
     assert torch.equal(acc, dw + dw)
     want, fast = d @ wv.T, U.product_bound_fast(np.abs(d) @ np.abs(wv).T, S)

@@ -23,7 +23,8 @@ def _declared(header):
 
 
 def test_headers_and_exports():
-    assert _declared("crisp_fp8.h") == ["crisp_fp8_linear", "crisp_fp8_linear_ws", "crisp_fp8_product", "crisp_fp8_quant"]
+    assert _declared("crisp_fp8.h") == ["crisp_fp8_linear", "crisp_fp8_linear_backward", "crisp_fp8_linear_backward_ws", "crisp_fp8_linear_ws",
+                                         "crisp_fp8_product", "crisp_fp8_quant"]
     assert _declared("crisp_adamw.h") == ["crisp_adamw_batch", "crisp_hybrid_mask"]
     src = '#include <stdio.h>\n#include <stddef.h>\n#include "crisp_fp8.h"\n#include "crisp_adamw.h"\nint main(void) {' \
           'printf("%zu %zu %zu %zu %zu %zu %zu\\n", sizeof(crisp_fp8_mat), offsetof(crisp_fp8_mat, kind), sizeof(crisp_adamw_tensor),' \
@@ -98,18 +99,38 @@ def test_product_refusals():
 
 def test_linear_refusals():
     L = fp8.lib()
-    need = L.crisp_fp8_linear_ws(16, 200)
-    assert need == 16 * (256 + 2 * 4)
+    need = L.crisp_fp8_linear_ws(70, 200)
+    assert need == 70 * (256 + 2 * 4)
+    assert L.crisp_fp8_linear_ws(16, 200) == 0 and L.crisp_fp8_linear_ws(16, 1025) == 16 * 9 * 132       # one launch up to 128 blocks
     assert L.crisp_fp8_linear_ws(0, 200) == 0 and L.crisp_fp8_linear_ws(16, -1) == 0 and L.crisp_fp8_linear_ws(1 << 27, 512) == 0
     W = _mat(64, 200, fp8.TILES)
 
-    def linear(X=FAKE, t=1, T=16, ldx=200, Y=FAKE, ldy=64, ws=FAKE, n=need):
+    def linear(X=FAKE, t=1, T=70, ldx=200, Y=FAKE, ldy=64, ws=FAKE, n=need):
         return L.crisp_fp8_linear(X, t, T, ldx, C.byref(W), Y, ldy, 1, None, ws, n, None)
     assert linear(X=None) == crisp.EINVAL and linear(Y=None) == crisp.EINVAL and linear(t=7) == crisp.EINVAL
     assert linear(T=0) == crisp.ESHAPE and linear(ldx=199) == crisp.ESHAPE and linear(ldy=63) == crisp.ESHAPE
     assert linear(ws=FAKE + 8) == crisp.EALIGN
     assert linear(ws=None) == crisp.EBUFSIZE and linear(n=need - 1) == crisp.EBUFSIZE
     assert L.crisp_fp8_linear(FAKE, 1, 16, 200, None, FAKE, 64, 1, None, FAKE, need, None) == crisp.EINVAL
+
+
+def test_linear_backward_refusals():
+    L = fp8.lib()
+    need = L.crisp_fp8_linear_backward_ws(70, 300)
+    assert need == (70 * 3 * 132 + 15) // 16 * 16 + 300 * 132 and L.crisp_fp8_linear_backward_ws(0, 5) == 0 and L.crisp_fp8_linear_backward_ws(5, -1) == 0
+    Xt, Wt = _mat(200, 70), _mat(200, 300, fp8.TILES)
+
+    def backward(dY=FAKE, t=1, T=70, S=300, ldg=300, Xt=Xt, Wt=Wt, dX=FAKE, lddx=200, dxt=1, dW=FAKE, lddw=200, dwt=0, acc=0, ws=FAKE, n=need):
+        return L.crisp_fp8_linear_backward(dY, t, T, S, ldg, C.byref(Xt) if Xt else None, C.byref(Wt) if Wt else None, dX, lddx, dxt,
+                                           dW, lddw, dwt, acc, ws, n, None)
+    for bad in (dict(dX=None, dW=None), dict(dY=None), dict(t=2), dict(Xt=None), dict(Wt=None), dict(acc=2), dict(dxt=2), dict(dwt=-1),
+                dict(Xt=_mat(200, 70, kind=2))):
+        assert backward(**bad) == crisp.EINVAL, bad
+    for bad in (dict(T=0), dict(S=0), dict(ldg=299), dict(T=71), dict(S=301, ldg=301), dict(Xt=_mat(201, 70)), dict(lddx=199), dict(lddw=199)):
+        assert backward(**bad) == crisp.ESHAPE, bad
+    for bad in (dict(dY=FAKE + 1), dict(dX=FAKE + 1), dict(dW=FAKE + 2), dict(ws=FAKE + 4)):
+        assert backward(**bad) == crisp.EALIGN, bad
+    assert backward(ws=None) == crisp.EBUFSIZE and backward(n=need - 1) == crisp.EBUFSIZE
 
 
 def _adamw(h=None, count=1, **k):
