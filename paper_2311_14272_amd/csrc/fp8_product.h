@@ -29,8 +29,8 @@ struct ProductArgs {
     int raw_bf16, raw_vec, K;
 };
 
-// Blocks of X that a workgroup of fp8_split_kernel quantises for itself.  Its 512 threads take 32 of them in 0.2 us; a launch of
-// the quantiser's own costs 2 us more on the GPU and 2 on the host.
+// Blocks of X that a workgroup of fp8_split_kernel quantises for itself.  Its 512 or 1024 threads take 32 or 64 of them in
+// 0.2 us; a launch of the quantiser's own costs 2 us more on the GPU and 3 on the host.
 constexpr int FP8_OWN_BLOCKS = 128;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));

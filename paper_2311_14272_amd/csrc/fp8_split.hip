@@ -8,8 +8,6 @@
 
 namespace crisp {
 
-constexpr int SPLIT_WAVES = 8;
-
 template <bool BF16>
 __device__ __forceinline__ f32x4 block_sum(const i32x4 (&w)[2], const i32x4 (&x)[2]) {
     f32x4 c = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -28,9 +26,9 @@ __device__ __forceinline__ f32x4 block_sum(const i32x4 (&w)[2], const i32x4 (&x)
 
 // U: blocks that a wave requests at a time.  RAW: X is not in 8 bits yet; the workgroup quantises it into LDS, all of it, while its
 // first weights are on their way (16 rows at most, and FP8_OWN_BLOCKS blocks).
-template <int MS, int MT, int U, bool BF16, bool TILES, bool RAW>
-__global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs a, int tiles_s) {
-    __shared__ f32x4 part[SPLIT_WAVES][MS * MT][64];
+template <int MS, int MT, int U, int WAVES, bool BF16, bool TILES, bool RAW>
+__global__ __launch_bounds__(64 * WAVES) void fp8_split_kernel(ProductArgs a, int tiles_s) {
+    __shared__ f32x4 part[WAVES][MS * MT][64];
     __shared__ __align__(16) uint8_t own_q[RAW ? FP8_OWN_BLOCKS * 128 : 16];
     __shared__ float own_s[RAW ? FP8_OWN_BLOCKS : 1];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -62,7 +60,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
     auto weights = [&](int b0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int b = min(b0 + u * SPLIT_WAVES, a.kb - 1);       // (behind the last block it is fetched again and left out)
+            const int b = min(b0 + u * WAVES, a.kb - 1);       // (behind the last block it is fetched again and left out)
 #pragma unroll
             for (int r = 0; r < MS; ++r) {
                 wv[u][r][0] = *reinterpret_cast<const i32x4*>(w[r] + (int64_t)b * 128);
@@ -81,7 +79,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
         weights(wave);
         __builtin_amdgcn_sched_barrier(0);
         const int blocks = a.T * a.kb;
-        for (int e0 = 0; e0 < blocks; e0 += 4 * SPLIT_WAVES) {
+        for (int e0 = 0; e0 < blocks; e0 += 4 * WAVES) {
             const int e = e0 + threadIdx.x / 16;
             if (e < blocks) {
                 const int t = e / a.kb, c = (e - t * a.kb) * 128 + threadIdx.x % 16 * 8;
@@ -95,13 +93,13 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
         __syncthreads();
     }
 
-    for (int b0 = wave; b0 < a.kb; b0 += U * SPLIT_WAVES) {
+    for (int b0 = wave; b0 < a.kb; b0 += U * WAVES) {
         i32x4 xv[U][MT][2];
         float f[U][MT];
         if (!RAW || b0 != wave) weights(b0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int b = min(b0 + u * SPLIT_WAVES, a.kb - 1);
+            const int b = min(b0 + u * WAVES, a.kb - 1);
 #pragma unroll
             for (int q = 0; q < MT; ++q) {
                 if constexpr (RAW) {
@@ -119,7 +117,7 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
         __builtin_amdgcn_sched_barrier(0);       // all requests first
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const bool there = b0 + u * SPLIT_WAVES < a.kb;
+            const bool there = b0 + u * WAVES < a.kb;
 #pragma unroll
             for (int r = 0; r < MS; ++r)
 #pragma unroll
@@ -139,11 +137,11 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
         for (int q = 0; q < MT; ++q) part[wave][r * MT + q][lane] = sum[r][q];
     __syncthreads();
     // thread (tile, lane): four consecutive results of a row
-    for (int e = threadIdx.x; e < MS * MT * 64; e += 64 * SPLIT_WAVES) {
+    for (int e = threadIdx.x; e < MS * MT * 64; e += 64 * WAVES) {
         const int tile = e / 64, l = e % 64;
         f32x4 y = part[0][tile][l];
 #pragma unroll
-        for (int v = 1; v < SPLIT_WAVES; ++v) y += part[v][tile][l];
+        for (int v = 1; v < WAVES; ++v) y += part[v][tile][l];
         const int t = t0 + tile % MT * 16 + l % 16, s = s0 + tile / MT * 16 + l / 16 * 4;
         if (t < a.T) {
 #pragma unroll
@@ -153,30 +151,24 @@ __global__ __launch_bounds__(64 * SPLIT_WAVES) void fp8_split_kernel(ProductArgs
     }
 }
 
-template <int MS, int MT, int U, bool RAW = false>
+template <int MS, int MT, int U, int WAVES, bool RAW = false>
 static void launch_split(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + 16 * MS - 1) / (16 * MS), tt = (a.T + 16 * MT - 1) / (16 * MT);
-    auto kernel = a.y_bf16 ? (a.w_tiles ? fp8_split_kernel<MS, MT, U, true, true, RAW> : fp8_split_kernel<MS, MT, U, true, false, RAW>)
-                           : (a.w_tiles ? fp8_split_kernel<MS, MT, U, false, true, RAW> : fp8_split_kernel<MS, MT, U, false, false, RAW>);
-    kernel<<<(unsigned)ts * (unsigned)tt, 64 * SPLIT_WAVES, 0, st>>>(a, ts);
+    auto kernel = a.y_bf16 ? (a.w_tiles ? fp8_split_kernel<MS, MT, U, WAVES, true, true, RAW> : fp8_split_kernel<MS, MT, U, WAVES, true, false, RAW>)
+                           : (a.w_tiles ? fp8_split_kernel<MS, MT, U, WAVES, false, true, RAW> : fp8_split_kernel<MS, MT, U, WAVES, false, false, RAW>);
+    kernel<<<(unsigned)ts * (unsigned)tt, 64 * WAVES, 0, st>>>(a, ts);
 }
 
-// Up to 16, 32 and 64 rows of X.  A wave requests four blocks at a time where there are more than two for each, else fewer
-// (what is requested behind the last block is fetched for nothing).
+// Up to 16, 32 and more rows of X.  Two blocks requested at a time: with four, 16 x 512 x 1152 takes 6.1 us instead of 4.4 (what
+// is requested behind the last block is fetched for nothing) and 4 x 4096 x 11008 16.0 instead of 14.7; 32 W rows a workgroup are
+// slower (1 x 4096 x 4096: 8.0 us against 6.9).  16 waves where they get two blocks each: 1 x 4096 x 4096 6.3 us against 6.9,
+// 13 x 11008 x 4096 14.1 against 14.9.
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st) {
-    const int each = (a.kb + SPLIT_WAVES - 1) / SPLIT_WAVES;
-    if (a.raw) {
-        if (each > 2) launch_split<1, 1, 4, true>(a, st);
-        else launch_split<1, 1, 2, true>(a, st);
-    } else if (a.T <= 16) {
-        if (each > 2) launch_split<1, 1, 4>(a, st);
-        else launch_split<1, 1, 2>(a, st);
-    } else if (a.T <= 32) {
-        if (each > 2) launch_split<1, 2, 4>(a, st);
-        else launch_split<1, 2, 2>(a, st);
-    } else {
-        launch_split<2, 2, 2>(a, st);
-    }
+    const bool many = a.kb >= 32;
+    if (a.raw) many ? launch_split<1, 1, 2, 16, true>(a, st) : launch_split<1, 1, 2, 8, true>(a, st);
+    else if (a.T <= 16) many ? launch_split<1, 1, 2, 16>(a, st) : launch_split<1, 1, 2, 8>(a, st);
+    else if (a.T <= 32) launch_split<1, 2, 2, 8>(a, st);
+    else launch_split<2, 2, 2, 8>(a, st);
     return hipGetLastError();
 }
 

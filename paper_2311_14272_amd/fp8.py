@@ -14,6 +14,7 @@ and serving is y = linear(x, w8).  Tensors live on the current device; work goes
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -29,6 +30,8 @@ class _Mat(C.Structure):
                 ("cols", C.c_int64), ("kind", C.c_int32), ("reserved", C.c_int32)]
 
 
+_pack = struct.Struct("@PPqqqqii").pack          # a crisp_fp8_mat as bytes: a third of the time of a ctypes structure
+
 _lib = None
 
 
@@ -36,7 +39,8 @@ def lib():
     global _lib
     if _lib is None:
         L = crisp.lib()
-        vp, i32, i64, mat = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(_Mat)
+        vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        mat = C.c_void_p            # bytes (Fp8Mat.c) or a pointer to a structure
         L.crisp_fp8_quant.argtypes = [vp, i32, i64, i64, i64, vp, mat, mat, vp]
         L.crisp_fp8_product.argtypes = [mat, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp]
         L.crisp_fp8_linear.argtypes = [vp, i32, i64, i64, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp, C.c_size_t, vp]
@@ -77,21 +81,29 @@ class Fp8Mat:
         self._fill(q, scale, rows, cols, kind)
 
     def _fill(self, q, scale, rows, cols, kind):
-        want = scale.shape
         self.q, self.scale, self.rows, self.cols, self.kind = q, scale, rows, cols, kind
         # (a tensor of one row may carry any row stride)
-        self.c = _Mat(_here(q, "q"), _here(scale, "scale"), q.stride(0) if rows > 1 else max(q.stride(0), q.shape[1]),
-                      scale.stride(0) if want[0] > 1 else max(scale.stride(0), want[1]), rows, cols, kind, 0)
+        self.c = _pack(_here(q, "q"), _here(scale, "scale"), q.stride(0) if rows > 1 else max(q.stride(0), q.shape[1]),
+                       scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1]), rows, cols, kind, 0)
+
+
+def _new(rows, cols, kind, device):
+    b = (cols + 127) >> 7
+    out = Fp8Mat.__new__(Fp8Mat)
+    out.q = q = torch.empty_strided((rows, b << 7), (b << 7, 1), dtype=torch.float8_e4m3fn, device=device)      # (0.4 us less than empty)
+    shape = (b, rows) if kind == ROWS else ((rows + 127) >> 7, b)
+    out.scale = scale = torch.empty_strided(shape, (shape[1], 1), dtype=torch.float32, device=device)
+    out.rows, out.cols, out.kind = rows, cols, kind
+    out.c = _pack(q.data_ptr(), scale.data_ptr(), b << 7, shape[1], rows, cols, kind, 0)
+    return out
 
 
 def alloc_mat(rows, cols, kind=ROWS, device="cuda") -> Fp8Mat:
     """Buffers of a rows x cols matrix in 8 bits, to be filled by quantize."""
     if kind not in (ROWS, TILES) or rows < 1 or cols < 1:
         raise ValueError("a matrix of at least 1 x 1, kind ROWS or TILES")
-    b = _blocks(cols)
-    q = torch.empty((rows, b * BLOCK), dtype=torch.float8_e4m3fn, device=device)
-    out = Fp8Mat.__new__(Fp8Mat)
-    out._fill(q, torch.empty((b, rows) if kind == ROWS else (_blocks(rows), b), dtype=torch.float32, device=device), rows, cols, kind)
+    out = _new(rows, cols, kind, device)
+    _here(out.q, "the matrix")
     return out
 
 
@@ -100,16 +112,18 @@ def _input(x):
     if x.dim() != 2 or x.dtype not in _IN or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("a matrix of fp32 or bf16 with contiguous rows is wanted")
     rows, cols = x.shape
+    if rows < 1 or cols < 1:
+        raise ValueError("a matrix of at least 1 x 1 is wanted")
     return _here(x, "input"), _IN[x.dtype], rows, cols, x.stride(0) if rows > 1 else max(x.stride(0), cols)
 
 
-def _quant(x, mask, out, out_t):
-    p, kind, rows, cols, ldx = _input(x)
-    if mask is not None and (mask.dtype != torch.int32 or not mask.is_contiguous() or mask.numel() < rows * (-(-cols // 32))):
-        raise ValueError("mask: rows x ceil(cols/32) contiguous int32 words")
-    st = lib().crisp_fp8_quant(p, kind, rows, cols, ldx, None if mask is None else _here(mask, "mask"),
-                               C.byref(out.c) if out is not None else None, C.byref(out_t.c) if out_t is not None else None,
-                               crisp._stream())
+def _quant(x, mask, out, out_t, inp=None):
+    p, t, rows, cols, ldx = inp or _input(x)
+    if mask is not None:
+        if mask.dtype != torch.int32 or not mask.is_contiguous() or mask.numel() < rows * (-(-cols // 32)):
+            raise ValueError("mask: rows x ceil(cols/32) contiguous int32 words")
+        mask = _here(mask, "mask")
+    st = (_lib or lib()).crisp_fp8_quant(p, t, rows, cols, ldx, mask, out and out.c, out_t and out_t.c, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_quant", st)
 
@@ -117,22 +131,27 @@ def _quant(x, mask, out, out_t):
 def quantize(x, kind=ROWS, mask=None, out=None) -> Fp8Mat:
     """crisp_fp8_quant of x (fp32 or bf16) into out, allocated when not given.  mask: words as crisp.DeviceLayer.nm_mask or
     adamw.hybrid_mask hold them; positions whose bit is not set count as zero."""
-    out = alloc_mat(x.shape[0], x.shape[1], kind, x.device) if out is None else out
-    _quant(x, mask, out, None)
+    inp = _input(x)
+    if out is None:
+        out = _new(inp[2], inp[3], kind, x.device)
+    _quant(x, mask, out, None, inp)
     return out
 
 
 def quantize_both(x, kind=ROWS, mask=None, out=None, out_t=None):
     """(x, its transpose) in 8 bits, in one pass over x."""
-    out = alloc_mat(x.shape[0], x.shape[1], kind, x.device) if out is None else out
-    out_t = alloc_mat(x.shape[1], x.shape[0], kind, x.device) if out_t is None else out_t
-    _quant(x, mask, out, out_t)
+    inp = _input(x)
+    if out is None:
+        out = _new(inp[2], inp[3], kind, x.device)
+    if out_t is None:
+        out_t = _new(inp[3], inp[2], kind, x.device)
+    _quant(x, mask, out, out_t, inp)
     return out, out_t
 
 
 def _output(T, S, out, out_dtype, device):
     if out is None:
-        return torch.empty((T, S), dtype=out_dtype, device=device)
+        return torch.empty_strided((T, S), (S, 1), dtype=out_dtype, device=device)
     if out.dtype not in _IN or tuple(out.shape) != (T, S) or (S > 1 and out.stride(1) != 1):
         raise ValueError("out: %d x %d of fp32 or bf16 with contiguous rows" % (T, S))
     return out
@@ -157,7 +176,7 @@ def product(x: Fp8Mat, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None,
     per column of the result."""
     out = _output(x.rows, w.rows, out, out_dtype, x.q.device)
     ep = _epilogue(ep, bias, w.rows)
-    st = lib().crisp_fp8_product(C.byref(x.c), C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
+    st = (_lib or lib()).crisp_fp8_product(x.c, w.c, _here(out, "out"), _ld(out), _IN[out.dtype],
                                  C.byref(ep) if ep is not None else None, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_product", st)
@@ -172,11 +191,11 @@ def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None,
         raise ValueError("x has %d columns, the weights %d" % (K, w.cols))
     out = _output(T, w.rows, out, out_dtype, x.device)
     ep = _epilogue(ep, bias, w.rows)
-    L = lib()
+    L = _lib or lib()
     if ws is None:
         need = L.crisp_fp8_linear_ws(T, K)
         ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    st = L.crisp_fp8_linear(p, kind, T, ldx, C.byref(w.c), _here(out, "out"), _ld(out), _IN[out.dtype],
+    st = L.crisp_fp8_linear(p, kind, T, ldx, w.c, _here(out, "out"), _ld(out), _IN[out.dtype],
                             C.byref(ep) if ep is not None else None, None if ws is None else _here(ws, "ws"),
                             0 if ws is None else ws.numel() * ws.element_size(), crisp._stream())
     if st != crisp.OK:
@@ -194,7 +213,7 @@ def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=F
         raise ValueError("dy is %d x %d, x^T has %s columns, W^T %s" % (T, S, x_t and x_t.cols, w_t and w_t.cols))
     if (accumulate and dw is None) or (dx is not None and w_t is None) or (dw is not None and x_t is None):
         raise ValueError("accumulate adds to a dw that is given; dx needs w_t, dw needs x_t")
-    L = lib()
+    L = _lib or lib()
     if w_t is not None:
         dx = _output(T, w_t.rows, dx, torch.bfloat16, dy.device)
     if x_t is not None:
@@ -202,7 +221,7 @@ def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=F
     if ws is None:
         ws = torch.empty(max(16, L.crisp_fp8_linear_backward_ws(T, S)), dtype=torch.uint8, device=dy.device)
     none = (None, 0, 0)
-    st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, None if x_t is None else C.byref(x_t.c), None if w_t is None else C.byref(w_t.c),
+    st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, x_t and x_t.c, w_t and w_t.c,
                                      *(none if dx is None else (_here(dx, "dx"), _ld(dx), _IN[dx.dtype])),
                                      *(none if dw is None else (_here(dw, "dw"), _ld(dw), _IN[dw.dtype])), int(accumulate),
                                      _here(ws, "ws"), ws.numel() * ws.element_size(), crisp._stream())
