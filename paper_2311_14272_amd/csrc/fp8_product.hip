@@ -17,9 +17,9 @@ hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, vo
                               const crisp_epilogue* ep, hipStream_t st) {
     ProductArgs a = args_of(W, X.rows, Y, ldy, y_type, ep);
     a.x = X.q; a.xs = X.scale; a.ldx = X.ld; a.ldxs = X.lds;
-    // Up to 64 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us: 16 rows 6.5
-    // against 12 with 64 x 64 tiles, 32: 9.2 and 12.3, 64: 11.7 and 13.5, 128: 18.9 and 13.3).  So is a W of few rows: X is then
-    // what is read.  The tiled kernels' offsets inside a tile are 32 bits.
+    // Up to 32 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us, from memory: 16
+    // rows 6.5 against 12 with 64 x 64 tiles, 32: 9.2 and 11.7, 64: 12.6 and 13.0, 128: 18.9 and 12.7; from the caches 64: 10.7 and
+    // 9.4).  So is a W of few rows: X is then what is read.  The tiled kernels' offsets inside a tile are 32 bits.
     if (fp8_takes_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw)) return launch_fp8_split(a, st);
     return launch_fp8_tiled(a, st);
 }

@@ -159,7 +159,7 @@ static void launch_split(const ProductArgs& a, hipStream_t st) {
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * WAVES, 0, st>>>(a, ts);
 }
 
-// Up to 16, 32 and more rows of X.  Two blocks requested at a time: with four, 16 x 512 x 1152 takes 6.1 us instead of 4.4 (what
+// Up to 16, up to 32, and more rows of X.  Two blocks requested at a time: with four, 16 x 512 x 1152 takes 6.1 us instead of 4.4 (what
 // is requested behind the last block is fetched for nothing) and 4 x 4096 x 11008 16.0 instead of 14.7; 32 W rows a workgroup are
 // slower (1 x 4096 x 4096: 8.0 us against 6.9).  16 waves where they get two blocks each: 1 x 4096 x 4096 6.3 us against 6.9,
 // 13 x 11008 x 4096 14.1 against 14.9.

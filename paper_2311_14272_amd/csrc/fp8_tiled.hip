@@ -70,10 +70,11 @@ __global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * N
     constexpr int SC = LS * NW * 64;
     static_assert(BS % (8 * NW) == 0 && BT % (8 * NW) == 0 && BS % 64 == 0, "whole requests");
     constexpr int PER = LW + LX + LS;
-    constexpr int W = KG * BS * 128, X = KG * BT * 128;
-    __shared__ __align__(16) uint8_t w0[W], x0[X], w1[W], x1[X];
-    __shared__ __align__(16) uint8_t w2[STAGES > 2 ? W : 16], x2[STAGES > 2 ? X : 16], w3[STAGES > 3 ? W : 16], x3[STAGES > 3 ? X : 16];
-    __shared__ __align__(16) float s0_[KG * SC], s1_[KG * SC], s2_[STAGES > 2 ? KG * SC : 4], s3_[STAGES > 3 ? KG * SC : 4];
+    // One object a stage: W's rows, X's rows, scales.  The compiler tells requests to LDS apart by the object that they write, and
+    // no more than eight of them, and follows few address steps from an object: every address below is an object and one offset.
+    // Where it cannot tell, a read of LDS waits for all requests.
+    constexpr int W = KG * BS * 128, X = KG * BT * 128, STAGE = W + X + KG * SC * 4;
+    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16], st3[STAGES > 3 ? STAGE : 16];
     const int lane = threadIdx.x % 64, all = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wave = all % NW, kg = all / NW;                    // (kg is 0 where there is one group)
 
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * N
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         wr[c] = (kg * BS + ws * RS * 32 + si) * 128 + ((4 * h + c) ^ w_swizzle(si)) * 16;
-        xr[c] = (kg * BT + wt * RT * 32 + i) * 128 + ((4 * h + c) ^ x_swizzle(i)) * 16;
+        xr[c] = W + (kg * BT + wt * RT * 32 + i) * 128 + ((4 * h + c) ^ x_swizzle(i)) * 16;
     }
 
     f32x16 acc[RS][RT];
@@ -131,117 +132,146 @@ __global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * N
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][q][j] = 0.0f;
 
-    // request n of a step's PER
-    auto request = [&](int n, int b, uint8_t* wl, uint8_t* xl, float* sl) {
-        if (n < LS) {
+    // request n of a step's PER.  Rows of W and X through buffer descriptors of the tile: the lane's offset stays, the block's goes
+    // into the scalar one.
+    const __amdgpu_buffer_rsrc_t wd = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wb), 0, -1, 0x00027000);
+    const __amdgpu_buffer_rsrc_t xd = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(xb), 0, -1, 0x00027000);
+    auto request = [&](int n, int b, uint8_t* to) {
+        if (n < LW) {
             const int j = n;
-            __builtin_amdgcn_global_load_lds((global_ptr)(sp[j] + b * sstep[j]), (lds_ptr)(sl + kg * SC + (wave + j * NW) * 64), 4, 0, 0);
-        } else if (n < LS + LW) {
-            const int j = n - LS;
-            __builtin_amdgcn_global_load_lds((global_ptr)(wb + (int64_t)b * 128 + wo[j]), (lds_ptr)(wl + (kg * (BS / 8) + wave + j * NW) * 1024), 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(wd, (lds_ptr)(to + ((kg * (BS / 8) + wave + j * NW) * 1024)), 16, (int)wo[j], b * 128, 0, 0);
+        } else if (n < LW + LX) {
+            const int j = n - LW;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(xd, (lds_ptr)(to + (W + (kg * (BT / 8) + wave + j * NW) * 1024)), 16, (int)xo[j], b * 128, 0, 0);
         } else {
-            const int j = n - LS - LW;
-            __builtin_amdgcn_global_load_lds((global_ptr)(xb + (int64_t)b * 128 + xo[j]), (lds_ptr)(xl + (kg * (BT / 8) + wave + j * NW) * 1024), 16, 0, 0);
+            const int j = n - LW - LX;
+            __builtin_amdgcn_global_load_lds((global_ptr)(sp[j] + b * sstep[j]), (lds_ptr)(to + (W + X + (kg * SC + (wave + j * NW) * 64) * 4)), 4, 0, 0);
         }
     };
-    auto fetch = [&](int b, uint8_t* wl, uint8_t* xl, float* sl) {
+    auto fetch = [&](int b, uint8_t* to) {
 #pragma unroll
-        for (int n = 0; n < PER; ++n) request(n, b, wl, xl, sl);
+        for (int n = 0; n < PER; ++n) request(n, b, to);
     };
 
-    auto compute = [&](const uint8_t* wl, const uint8_t* xl, const float* sl, auto part) {
+    const int xscale = W + X + 4 * (kg * SC + BS + wt * RT * 32 + i), wscales = W + X + 4 * (kg * SC + ws * RS * 32 + (TILES ? 0 : 16 * h));
+    auto compute = [&](const uint8_t* st, auto part) {
         i32x4 xv[RT][4], wv[4];
         float f[RT];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            wv[c] = *reinterpret_cast<const i32x4*>(wl + wr[c]);
-            xv[0][c] = *reinterpret_cast<const i32x4*>(xl + xr[c]);
+            wv[c] = *reinterpret_cast<const i32x4*>(st + wr[c]);
+            xv[0][c] = *reinterpret_cast<const i32x4*>(st + xr[c]);
         }
 #pragma unroll
         for (int q = 1; q < RT; ++q)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) xv[q][c] = *reinterpret_cast<const i32x4*>(xl + xr[c] + q * 4096);
+            for (int c = 0; c < 4; ++c) xv[q][c] = *reinterpret_cast<const i32x4*>(st + (xr[c] + q * 4096));
 #pragma unroll
-        for (int q = 0; q < RT; ++q) f[q] = sl[kg * SC + BS + (wt * RT + q) * 32 + i];
-        const float wscale = TILES ? sl[kg * SC + ws * RS * 32] : 0.0f;
+        for (int q = 0; q < RT; ++q) f[q] = *reinterpret_cast<const float*>(st + (xscale + q * 128));
+        const float wscale = TILES ? *reinterpret_cast<const float*>(st + wscales) : 0.0f;
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 xw[BF16 ? 1 : RT][8];
-        if constexpr (!BF16) {
-#pragma unroll
-            for (int q = 0; q < RT; ++q)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    xw[q][2 * c] = widen(xv[q][c][0], xv[q][c][1]);
-                    xw[q][2 * c + 1] = widen(xv[q][c][2], xv[q][c][3]);
-                }
-        }
-        f32x16 p[2];
         f32x4 wsv[4];
         const f32x16 zero = {};
-        // the matrix cores are a tile ahead of the sums that enter the accumulators
+        if constexpr (BF16) {
+            // the matrix cores are a tile ahead of the sums that enter the accumulators
+            f32x16 p[2];
 #pragma unroll
-        for (int k = 0; k <= RS * RT; ++k) {
-            if (k < RS * RT) {
-                const int r = k / RT, q = k % RT;
-                if constexpr (BF16) {
+            for (int k = 0; k <= RS * RT; ++k) {
+                if (k < RS * RT) {
+                    const int r = k / RT, q = k % RT;
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
                         const i32x8 wa = __builtin_shufflevector(wv[2 * u], wv[2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
                         const i32x8 xa = __builtin_shufflevector(xv[q][2 * u], xv[q][2 * u + 1], 0, 1, 2, 3, 4, 5, 6, 7);
                         p[k % 2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, xa, u ? p[k % 2] : zero, 0, 0, 0, 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (q == RT - 1 && r + 1 < RS) {
+#pragma unroll
+                            for (int c = 2 * u; c < 2 * u + 2; ++c) wv[c] = *reinterpret_cast<const i32x4*>(st + (wr[c] + (r + 1) * 4096));
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
                     }
-                } else {
+                    if (TILES && k == 0) {
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const bf16x8 wa = widen(wv[u / 2][u % 2 * 2], wv[u / 2][u % 2 * 2 + 1]);
-                        p[k % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, xw[q][u], u ? p[k % 2] : zero, 0, 0, 0);
+                        for (int e = 0; e < RT; ++e) f[e] *= wscale;
                     }
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                if (TILES && k == 0) {
-#pragma unroll
-                    for (int e = 0; e < RT; ++e) f[e] *= wscale;
-                }
-                if (q == RT - 1 && r + 1 < RS) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) wv[c] = *reinterpret_cast<const i32x4*>(wl + wr[c] + (r + 1) * 4096);
+                    part(k);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                part(k);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            if (k > 0) {
-                const int r = (k - 1) / RT, q = (k - 1) % RT;
-                if (!TILES && q == 0) {
+                if (k > 0) {
+                    const int r = (k - 1) / RT, q = (k - 1) % RT;
+                    if (!TILES && q == 0) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(sl + kg * SC + (ws * RS + r) * 32 + 16 * h + 4 * c);
+                        for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(st + (wscales + r * 128 + 16 * c));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        } else {
+            // a row of tiles ahead; an eighth of the widening and of the sums goes between any two steps of the instruction
+            f32x16 p[2][RT];
+            bf16x8 xw[RT][8];
+#pragma unroll
+            for (int r = 0; r <= RS; ++r) {
+                if (!TILES && r > 0) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(st + (wscales + (r - 1) * 128 + 16 * c));
                 }
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int u = 0; u < 8; ++u) {
+                    if (r < RS) {
+                        const bf16x8 wa = widen(wv[u / 2][u % 2 * 2], wv[u / 2][u % 2 * 2 + 1]);
+#pragma unroll
+                        for (int q = 0; q < RT; ++q) {
+                            if (r == 0) xw[q][u] = widen(xv[q][u / 2][u % 2 * 2], xv[q][u / 2][u % 2 * 2 + 1]);
+                            p[r % 2][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, xw[q][u], u ? p[r % 2][q] : zero, 0, 0, 0);
+                        }
+                        if (u % 2 == 1 && r + 1 < RS) wv[u / 2] = *reinterpret_cast<const i32x4*>(st + (wr[u / 2] + (r + 1) * 4096));
+                        if (u == 1 && r == 0 && TILES) {
+#pragma unroll
+                            for (int e = 0; e < RT; ++e) f[e] *= wscale;
+                        }
+                        if (u % (8 / RT) == 8 / RT - 1) part(r * RT + u / (8 / RT));
+                    }
+                    if (r > 0) {
+#pragma unroll
+                        for (int q = 0; q < RT; ++q)
+#pragma unroll
+                            for (int j = 2 * u; j < 2 * u + 2; ++j)
+                                acc[r - 1][q][j] = __builtin_fmaf(p[(r - 1) % 2][q][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r - 1][q][j]);
+                    }
+                    if (r < RS) __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
     };
 
     constexpr int AHEAD = STAGES - 1;
-    constexpr int SPREAD = STAGES == 2 ? (RS * RT + 1) / 2 : RS * RT;     // tiles of a step that its requests go between
+    // tiles of a step that its requests go between: with two stages they have to arrive by the next step (8192^3: 425 us for three
+    // eighths of the step, 423 for six, 440 for all)
+    constexpr int SPREAD = STAGES == 2 ? (RS * RT * 6 + 7) / 8 : RS * RT;
     // (behind the last block the requests repeat it, into places that nobody reads any more: a step is then free of branches)
 #define CRISP_STEP(k, here, there)                                                                                \
     {                                                                                                             \
-        const int step = step0 + k, b = step * KG + kg, ahead = min(b + AHEAD * KG, a.kb - 1);                    \
+        const int step = step0 + k, b = step * KG + kg;                                                           \
+        const int ahead = min(b + AHEAD * KG, a.kb - 1);                                                          \
         wait_loads<(AHEAD - 1) * PER>();                                                                          \
         __builtin_amdgcn_s_barrier();                                                                             \
         if (KG > 1 && b >= a.kb) break;               /* the last step may have no block for the later groups */  \
-        compute(w##here, x##here, s##here##_, [&](int tile) {                                                     \
+        compute(st##here, [&](int tile) {                                                                         \
             _Pragma("unroll") for (int n = 0; n < PER; ++n)                                                       \
-                if (n * SPREAD / PER == tile) request(n, ahead, w##there, x##there, s##there##_);                 \
+                if (n * SPREAD / PER == tile) request(n, ahead, st##there);                                       \
         });                                                                                                       \
         if (step + 1 >= steps) break;                                                                             \
     }
     const int steps = (a.kb + KG - 1) / KG;
-    fetch(min(kg, a.kb - 1), w0, x0, s0_);
-    if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), w1, x1, s1_);
-    if constexpr (AHEAD > 2) fetch(min(2 * KG + kg, a.kb - 1), w2, x2, s2_);
+    fetch(min(kg, a.kb - 1), st0);
+    if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), st1);
+    if constexpr (AHEAD > 2) fetch(min(2 * KG + kg, a.kb - 1), st2);
+    // (with requests under way at the loop's head the compiler would wait for all of them in each of its rounds)
+    wait_loads<0>();
     for (int step0 = 0;; step0 += STAGES) {
         if constexpr (STAGES == 2) {
             CRISP_STEP(0, 0, 1) CRISP_STEP(1, 1, 0)
@@ -254,8 +284,8 @@ __global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * N
 #undef CRISP_STEP
     wait_loads<0>();
     if constexpr (KG > 1) {
-        static_assert(W >= BS * BT * 4, "a group's sums fit one stage's rows of W");
-        f32x16* part = reinterpret_cast<f32x16*>(w0);
+        static_assert(STAGE >= BS * BT * 4, "a group's sums fit a stage");
+        f32x16* part = reinterpret_cast<f32x16*>(st0);
 #pragma unroll
         for (int g = 1; g < KG; ++g) {
             __syncthreads();
@@ -300,18 +330,18 @@ static void launch_tiles(const ProductArgs& a, hipStream_t st) {
 }
 
 // The tile: the fewest rounds of 256 workgroups (each takes a CU's LDS) times what a step of a block takes, in microseconds as
-// measured with S = K = 4096 and T = 128 .. 4096.  Results in fp32 have twice the matrix work and the widening, and no registers
-// left for 256 x 256.  W with a scale for each row costs registers too (256 x 256 spills).
+// measured with S = K = 4096.  Results in fp32 have twice the matrix work and the widening, and no registers left for 256 x 256.
+// W with a scale for each row costs registers too (256 x 256 spills).
 //
-//   T of S = K = 4096, bf16, us:   128    256    512   1024   2048   4096
-//   64 x 64, two groups           13.3   13.5   24.2   48     94
-//   128 x 64, two groups          17.5   17.3   17.8   33.5   65.7
-//   128 x 128                     24.3   24.3   24.4   25.3   49.6
-//   128 x 256                                   32.8   33.4   38.6   70
-//   256 x 256                                                 62     61
+//   T of S = K = 4096, bf16, us:   256    512   1024   2048   4096   8192
+//   64 x 64, two groups           10.3     24     46     89    158    294
+//   128 x 64, two groups            17   14.6     34     66    117    220
+//   128 x 128                                   22.2     47     94    175
+//   128 x 256                                     32   36.5     74    148
+//   256 x 256                                            53     64    119
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
     static const struct { int bs, bt; float step[2]; } shapes[] = {         // [BF16]
-        {64, 64, {0.45f, 0.40f}}, {128, 64, {0.65f, 0.53f}}, {128, 128, {1.2f, 0.76f}}, {128, 256, {2.15f, 1.15f}}, {256, 256, {0.0f, 1.9f}}};
+        {64, 64, {0.49f, 0.32f}}, {128, 64, {0.82f, 0.46f}}, {128, 128, {1.45f, 0.69f}}, {128, 256, {2.3f, 1.14f}}, {256, 256, {0.0f, 2.0f}}};
     int best = 0;
     float least = 0.0f;
     for (int k = 0; k < 5; ++k) {

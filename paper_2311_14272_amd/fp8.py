@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
+from functools import lru_cache
 
 import torch
 
@@ -32,6 +33,8 @@ class _Mat(C.Structure):
 
 _pack = struct.Struct("@PPqqqqii").pack          # a crisp_fp8_mat as bytes: a third of the time of a ctypes structure
 
+_pack_ep = struct.Struct("@PPPqii").pack         # and a crisp_epilogue
+
 _lib = None
 
 
@@ -40,10 +43,10 @@ def lib():
     if _lib is None:
         L = crisp.lib()
         vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
-        mat = C.c_void_p            # bytes (Fp8Mat.c) or a pointer to a structure
+        mat = ep = C.c_void_p       # bytes (Fp8Mat.c) or a pointer to a structure
         L.crisp_fp8_quant.argtypes = [vp, i32, i64, i64, i64, vp, mat, mat, vp]
-        L.crisp_fp8_product.argtypes = [mat, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp]
-        L.crisp_fp8_linear.argtypes = [vp, i32, i64, i64, mat, vp, i64, i32, C.POINTER(crisp.Epilogue), vp, C.c_size_t, vp]
+        L.crisp_fp8_product.argtypes = [mat, mat, vp, i64, i32, ep, vp]
+        L.crisp_fp8_linear.argtypes = [vp, i32, i64, i64, mat, vp, i64, i32, ep, vp, C.c_size_t, vp]
         L.crisp_fp8_linear_backward.argtypes = [vp, i32, i64, i64, i64, mat, mat, vp, i64, i32, vp, i64, i32, i32, vp, C.c_size_t, vp]
         for f in (L.crisp_fp8_quant, L.crisp_fp8_product, L.crisp_fp8_linear, L.crisp_fp8_linear_backward):
             f.restype = i32
@@ -53,11 +56,28 @@ def lib():
     return _lib
 
 
+@lru_cache(maxsize=1024)
+def _linear_ws(T, K):
+    return lib().crisp_fp8_linear_ws(T, K)
+
+
+@lru_cache(maxsize=1024)
+def _backward_ws(T, S):
+    return lib().crisp_fp8_linear_backward_ws(T, S)
+
+
 def _here(t, what):
     """A tensor's address; it has to be on the device whose stream the work goes to."""
     if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
         raise ValueError("%s is on %s, not on the current GPU" % (what, t.device))
     return t.data_ptr()
+
+
+def _mats_here(*mats):
+    now = torch._C._cuda_getDevice()
+    for m in mats:
+        if m is not None and m.dev != now:
+            raise ValueError("a matrix is on GPU %d, not on the current one" % m.dev)
 
 
 def _blocks(n):
@@ -68,7 +88,7 @@ class Fp8Mat:
     """A rows x cols matrix in 8 bits over existing tensors: q, rows x at least round_up(cols, 128) bytes (uint8 or
     float8_e4m3fn, zeros behind the columns), and scale, fp32, ceil(cols/128) x rows (ROWS) or ceil(rows/128) x ceil(cols/128)
     (TILES); both with contiguous rows, any row stride that the header allows.  Keeps the tensors alive."""
-    __slots__ = ("q", "scale", "rows", "cols", "kind", "c")
+    __slots__ = ("q", "scale", "rows", "cols", "kind", "c", "dev")
 
     def __init__(self, q, scale, rows, cols, kind):
         if kind not in (ROWS, TILES):
@@ -81,7 +101,7 @@ class Fp8Mat:
         self._fill(q, scale, rows, cols, kind)
 
     def _fill(self, q, scale, rows, cols, kind):
-        self.q, self.scale, self.rows, self.cols, self.kind = q, scale, rows, cols, kind
+        self.q, self.scale, self.rows, self.cols, self.kind, self.dev = q, scale, rows, cols, kind, q.get_device()
         # (a tensor of one row may carry any row stride)
         self.c = _pack(_here(q, "q"), _here(scale, "scale"), q.stride(0) if rows > 1 else max(q.stride(0), q.shape[1]),
                        scale.stride(0) if scale.shape[0] > 1 else max(scale.stride(0), scale.shape[1]), rows, cols, kind, 0)
@@ -93,7 +113,7 @@ def _new(rows, cols, kind, device):
     out.q = q = torch.empty_strided((rows, b << 7), (b << 7, 1), dtype=torch.float8_e4m3fn, device=device)      # (0.4 us less than empty)
     shape = (b, rows) if kind == ROWS else ((rows + 127) >> 7, b)
     out.scale = scale = torch.empty_strided(shape, (shape[1], 1), dtype=torch.float32, device=device)
-    out.rows, out.cols, out.kind = rows, cols, kind
+    out.rows, out.cols, out.kind, out.dev = rows, cols, kind, q.get_device()
     out.c = _pack(q.data_ptr(), scale.data_ptr(), b << 7, shape[1], rows, cols, kind, 0)
     return out
 
@@ -119,6 +139,7 @@ def _input(x):
 
 def _quant(x, mask, out, out_t, inp=None):
     p, t, rows, cols, ldx = inp or _input(x)
+    _mats_here(out, out_t)
     if mask is not None:
         if mask.dtype != torch.int32 or not mask.is_contiguous() or mask.numel() < rows * (-(-cols // 32)):
             raise ValueError("mask: rows x ceil(cols/32) contiguous int32 words")
@@ -158,13 +179,14 @@ def _output(T, S, out, out_dtype, device):
 
 
 def _epilogue(ep, bias, S):
+    """What the library takes: NULL, or a structure."""
     if bias is None:
-        return ep
+        return None if ep is None else C.byref(ep)
     if ep is not None:
         raise ValueError("bias goes into the epilogue when there is one")
     if bias.dtype != torch.float32 or bias.dim() != 1 or bias.numel() != S or (S > 1 and bias.stride(0) != 1):
         raise ValueError("bias: %d contiguous fp32 values" % S)
-    return crisp.Epilogue(None, _here(bias, "bias"), None, 0, 0, 0)
+    return _pack_ep(0, _here(bias, "bias"), 0, 0, 0, 0)
 
 
 def _ld(y):
@@ -174,10 +196,10 @@ def _ld(y):
 def product(x: Fp8Mat, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None):
     """crisp_fp8_product: x w^T, x.rows x w.rows; into out, allocated as out_dtype when not given.  ep: crisp.epilogue(...),
     per column of the result."""
+    _mats_here(x, w)
     out = _output(x.rows, w.rows, out, out_dtype, x.q.device)
     ep = _epilogue(ep, bias, w.rows)
-    st = (_lib or lib()).crisp_fp8_product(x.c, w.c, _here(out, "out"), _ld(out), _IN[out.dtype],
-                                 C.byref(ep) if ep is not None else None, crisp._stream())
+    st = (_lib or lib()).crisp_fp8_product(x.c, w.c, _here(out, "out"), _ld(out), _IN[out.dtype], ep, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_product", st)
     return out
@@ -189,15 +211,15 @@ def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None,
     p, kind, T, K, ldx = _input(x)
     if K != w.cols:
         raise ValueError("x has %d columns, the weights %d" % (K, w.cols))
+    _mats_here(w)
     out = _output(T, w.rows, out, out_dtype, x.device)
     ep = _epilogue(ep, bias, w.rows)
-    L = _lib or lib()
     if ws is None:
-        need = L.crisp_fp8_linear_ws(T, K)
+        need = _linear_ws(T, K)
         ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    st = L.crisp_fp8_linear(p, kind, T, ldx, w.c, _here(out, "out"), _ld(out), _IN[out.dtype],
-                            C.byref(ep) if ep is not None else None, None if ws is None else _here(ws, "ws"),
-                            0 if ws is None else ws.numel() * ws.element_size(), crisp._stream())
+    st = (_lib or lib()).crisp_fp8_linear(p, kind, T, ldx, w.c, _here(out, "out"), _ld(out), _IN[out.dtype], ep,
+                                          None if ws is None else _here(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
+                                          crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_linear", st)
     return out
@@ -213,13 +235,14 @@ def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=F
         raise ValueError("dy is %d x %d, x^T has %s columns, W^T %s" % (T, S, x_t and x_t.cols, w_t and w_t.cols))
     if (accumulate and dw is None) or (dx is not None and w_t is None) or (dw is not None and x_t is None):
         raise ValueError("accumulate adds to a dw that is given; dx needs w_t, dw needs x_t")
+    _mats_here(x_t, w_t)
     L = _lib or lib()
     if w_t is not None:
         dx = _output(T, w_t.rows, dx, torch.bfloat16, dy.device)
     if x_t is not None:
         dw = _output(S, x_t.rows, dw, torch.float32, dy.device)
     if ws is None:
-        ws = torch.empty(max(16, L.crisp_fp8_linear_backward_ws(T, S)), dtype=torch.uint8, device=dy.device)
+        ws = torch.empty(max(16, _backward_ws(T, S)), dtype=torch.uint8, device=dy.device)
     none = (None, 0, 0)
     st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, x_t and x_t.c, w_t and w_t.c,
                                      *(none if dx is None else (_here(dx, "dx"), _ld(dx), _IN[dx.dtype])),
