@@ -140,8 +140,9 @@ crisp_status crisp_fp8_linear_backward(const void* dY, int32_t in_type, int64_t 
     if (!ws || ws_bytes < crisp_fp8_linear_backward_ws(T, S)) return CRISP_EBUFSIZE;
     const crisp_fp8_mat g = mat_in(ws, T, S), gt = mat_in(static_cast<uint8_t*>(ws) + mat_bytes(T, S), S, T);
     hipError_t e = launch_fp8_quant(dY, in_type, T, S, ldg, nullptr, dX ? &g : nullptr, dW ? &gt : nullptr, (hipStream_t)stream);
-    if (e == hipSuccess && dX) e = launch_fp8_product(g, *Wt, dX, lddx, dx_type, nullptr, (hipStream_t)stream);
-    if (e == hipSuccess && dW) e = launch_fp8_product(gt, *Xt, dW, lddw, dw_type, ep, (hipStream_t)stream);
+    if (e == hipSuccess && dX && dW) e = launch_fp8_gradients(g, *Wt, dX, lddx, dx_type, gt, *Xt, dW, lddw, dw_type, ep, (hipStream_t)stream);
+    else if (e == hipSuccess && dX) e = launch_fp8_product(g, *Wt, dX, lddx, dx_type, nullptr, (hipStream_t)stream);
+    else if (e == hipSuccess) e = launch_fp8_product(gt, *Xt, dW, lddw, dw_type, ep, (hipStream_t)stream);
     return e == hipSuccess ? CRISP_OK : CRISP_EDEVICE;
 }
 

@@ -13,6 +13,10 @@ inline bool fp8_takes_split(int64_t T, int64_t S, int64_t ld) { return T <= 32 |
 hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
                               const crisp_epilogue* ep, hipStream_t st);
 
+// Both gradients of a layer: dX = G Wt^T and dW = Gt Xt^T (ep: dW's).
+hipError_t launch_fp8_gradients(const crisp_fp8_mat& G, const crisp_fp8_mat& Wt, void* dX, int64_t lddx, int dx_type, const crisp_fp8_mat& Gt,
+                                const crisp_fp8_mat& Xt, void* dW, int64_t lddw, int dw_type, const crisp_epilogue* ep, hipStream_t st);
+
 // The layer from X as it is, in one launch: whether it takes these sizes, and the launch.
 bool fp8_takes_raw(int64_t T, int64_t K);
 hipError_t launch_fp8_raw(const void* X, int in_type, int64_t T, int64_t ldx, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,

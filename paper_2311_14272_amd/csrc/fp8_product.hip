@@ -13,15 +13,30 @@ static ProductArgs args_of(const crisp_fp8_mat& W, int64_t T, void* Y, int64_t l
     return a;
 }
 
-hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
-                              const crisp_epilogue* ep, hipStream_t st) {
+static ProductArgs args_of(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type, const crisp_epilogue* ep) {
     ProductArgs a = args_of(W, X.rows, Y, ldy, y_type, ep);
     a.x = X.q; a.xs = X.scale; a.ldx = X.ld; a.ldxs = X.lds;
-    // Up to 32 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us, from memory: 16
-    // rows 6.5 against 12 with 64 x 64 tiles, 32: 9.2 and 11.7, 64: 12.6 and 13.0, 128: 18.9 and 12.7; from the caches 64: 10.7 and
-    // 9.4).  So is a W of few rows: X is then what is read.  The tiled kernels' offsets inside a tile are 32 bits.
-    if (fp8_takes_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw)) return launch_fp8_split(a, st);
-    return launch_fp8_tiled(a, st);
+    return a;
+}
+
+static bool takes_split(const ProductArgs& a) { return fp8_takes_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw); }
+
+// Up to 32 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us, from memory: 16
+// rows 6.5 against 12 with 64 x 64 tiles, 32: 9.2 and 11.7, 64: 12.6 and 13.0, 128: 18.9 and 12.7; from the caches 64: 10.7 and
+// 9.4).  So is a W of few rows: X is then what is read.  The tiled kernels' offsets inside a tile are 32 bits.
+static hipError_t launch_product(const ProductArgs& a, hipStream_t st) { return takes_split(a) ? launch_fp8_split(a, st) : launch_fp8_tiled(a, st); }
+
+hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
+                              const crisp_epilogue* ep, hipStream_t st) {
+    return launch_product(args_of(X, W, Y, ldy, y_type, ep), st);
+}
+
+hipError_t launch_fp8_gradients(const crisp_fp8_mat& G, const crisp_fp8_mat& Wt, void* dX, int64_t lddx, int dx_type, const crisp_fp8_mat& Gt,
+                                const crisp_fp8_mat& Xt, void* dW, int64_t lddw, int dw_type, const crisp_epilogue* ep, hipStream_t st) {
+    const ProductArgs a = args_of(G, Wt, dX, lddx, dx_type, nullptr), b = args_of(Gt, Xt, dW, lddw, dw_type, ep);
+    if (!takes_split(a) && !takes_split(b) && fp8_pairs(a, b)) return launch_fp8_pair(a, b, st);
+    const hipError_t e = launch_product(a, st);
+    return e == hipSuccess ? launch_product(b, st) : e;
 }
 
 bool fp8_takes_raw(int64_t T, int64_t K) { return T <= 16 && T * ((K + FP8_BLOCK - 1) / FP8_BLOCK) <= FP8_OWN_BLOCKS; }

@@ -62,23 +62,29 @@ __device__ __forceinline__ void wait_loads() {
 // A step begins when its block has arrived for every wave (each waits for its own share, then all meet) - by then everybody
 // is done with the block before, whose place the next request takes.  All a wave's memory operations are requests to LDS,
 // the same number each step, so that the wait can leave the later steps' ones outstanding.
+//
+// One object of LDS a stage: W's rows, X's rows, scales.  The compiler tells requests to LDS apart by the object that they write,
+// no more than eight of them, and follows few address steps from an object: every address here is an object and one offset.  Where
+// it cannot tell, a read of LDS waits for all requests.
+template <int NS, int NT, int RS, int RT, int KG>
+struct Tiles {
+    static constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
+    static constexpr int LS = ((BS + BT) / 64 + NW - 1) / NW;    // requests of 64 scales that a wave makes per step (some may be nobody's)
+    static constexpr int SC = LS * NW * 64;
+    static constexpr int W = KG * BS * 128, X = KG * BT * 128, STAGE = W + X + KG * SC * 4;
+};
+
 template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
-__global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * NT == 4 ? 1 : 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
-    constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
+__device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s, int tiles_t, int id, uint8_t* st0, uint8_t* st1, uint8_t* st2,
+                                              uint8_t* st3) {
+    typedef Tiles<NS, NT, RS, RT, KG> G;
+    constexpr int NW = G::NW, BS = G::BS, BT = G::BT, LS = G::LS, SC = G::SC, W = G::W, X = G::X, STAGE = G::STAGE;
     constexpr int LW = BS / 8 / NW, LX = BT / 8 / NW;            // requests of eight rows that a wave makes per step
-    constexpr int LS = ((BS + BT) / 64 + NW - 1) / NW;           // and of 64 scales (some may be nobody's)
-    constexpr int SC = LS * NW * 64;
     static_assert(BS % (8 * NW) == 0 && BT % (8 * NW) == 0 && BS % 64 == 0, "whole requests");
     constexpr int PER = LW + LX + LS;
-    // One object a stage: W's rows, X's rows, scales.  The compiler tells requests to LDS apart by the object that they write, and
-    // no more than eight of them, and follows few address steps from an object: every address below is an object and one offset.
-    // Where it cannot tell, a read of LDS waits for all requests.
-    constexpr int W = KG * BS * 128, X = KG * BT * 128, STAGE = W + X + KG * SC * 4;
-    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16], st3[STAGES > 3 ? STAGE : 16];
     const int lane = threadIdx.x % 64, all = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wave = all % NW, kg = all / NW;                    // (kg is 0 where there is one group)
 
-    int id = blockIdx.x;
     const int n = tiles_s * tiles_t, per = n / XCDS;
     if (id < per * XCDS) id = id % XCDS * per + id / XCDS;
     const int in_group = GROUP * tiles_s, group = id / in_group, first = group * GROUP;
@@ -322,6 +328,23 @@ __global__ __launch_bounds__(64 * NS * NT * KG, KG == 1 && STAGES == 4 && NS * N
             store_y16<BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, acc[r][q], plain);
 }
 
+template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
+__global__ __launch_bounds__(64 * NS * NT * KG, 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
+    constexpr int STAGE = Tiles<NS, NT, RS, RT, KG>::STAGE;
+    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16], st3[STAGES > 3 ? STAGE : 16];
+    tiled_product<NS, NT, RS, RT, STAGES, KG, BF16, TILES>(a, tiles_s, tiles_t, (int)blockIdx.x, st0, st1, st2, st3);
+}
+
+// A layer's two gradients in one launch, the input's (bf16, W with a scale for 128 x 128) in the first workgroups, the weight's
+// (fp32, both operands with a scale for each row) in the others: for sizes whose 64 x 64 tiles leave CUs idle.
+__global__ __launch_bounds__(512, 2) void fp8_pair_kernel(ProductArgs a, ProductArgs b, int a_s, int a_t, int b_s, int b_t) {
+    constexpr int STAGE = Tiles<2, 2, 1, 1, 2>::STAGE;
+    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGE];
+    const int first = a_s * a_t;
+    if ((int)blockIdx.x < first) tiled_product<2, 2, 1, 1, 3, 2, true, true>(a, a_s, a_t, (int)blockIdx.x, st0, st1, st2, nullptr);
+    else tiled_product<2, 2, 1, 1, 3, 2, false, false>(b, b_s, b_t, (int)blockIdx.x - first, st0, st1, st2, nullptr);
+}
+
 template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16>
 static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + NS * RS * 32 - 1) / (NS * RS * 32), tt = (a.T + NT * RT * 32 - 1) / (NT * RT * 32);
@@ -339,7 +362,7 @@ static void launch_tiles(const ProductArgs& a, hipStream_t st) {
 //   128 x 128                                   22.2     47     94    175
 //   128 x 256                                     32   36.5     74    148
 //   256 x 256                                            53     64    119
-hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
+static int tile_shape(const ProductArgs& a) {
     static const struct { int bs, bt; float step[2]; } shapes[] = {         // [BF16]
         {64, 64, {0.49f, 0.32f}}, {128, 64, {0.82f, 0.46f}}, {128, 128, {1.45f, 0.69f}}, {128, 256, {2.3f, 1.14f}}, {256, 256, {0.0f, 2.0f}}};
     int best = 0;
@@ -350,6 +373,21 @@ hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
         const float cost = (float)((n + 255) / 256) * shapes[k].step[a.y_bf16];
         if (k == 0 || cost < least) { best = k; least = cost; }
     }
+    return best;
+}
+
+bool fp8_pairs(const ProductArgs& a, const ProductArgs& b) {
+    return a.y_bf16 && a.w_tiles && !b.y_bf16 && !b.w_tiles && tile_shape(a) == 0 && tile_shape(b) == 0;
+}
+
+hipError_t launch_fp8_pair(const ProductArgs& a, const ProductArgs& b, hipStream_t st) {
+    const int as = (a.S + 63) / 64, at = (a.T + 63) / 64, bs = (b.S + 63) / 64, bt = (b.T + 63) / 64;
+    fp8_pair_kernel<<<(unsigned)(as * at + bs * bt), 512, 0, st>>>(a, b, as, at, bs, bt);
+    return hipGetLastError();
+}
+
+hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
+    const int best = tile_shape(a);
     switch (best * 2 + a.y_bf16) {
         case 0: launch_tiles<2, 2, 1, 1, 3, 2, false>(a, st); break;
         case 1: launch_tiles<2, 2, 1, 1, 3, 2, true>(a, st); break;

@@ -302,6 +302,8 @@ def test_backward(shape):
     assert torch.equal(fp8.linear_backward(dy, None, w_t, dx=torch.empty((T, K), device="cuda"))[0], dx32)
     none, alone = fp8.linear_backward(dy, x_t, None)
     dy8, dy_t = fp8.quantize_both(dy)
+    both = fp8.linear_backward(dy, x_t, w_t)
+    assert torch.equal(both[0], fp8.product(dy8, w_t)) and torch.equal(both[1], dw)
     assert none is None and torch.equal(alone, dw) and torch.equal(fp8.product(dy_t, x_t, out_dtype=torch.float32), dw)
     again, acc = fp8.linear_backward(dy, x_t, w_t, dw=dw.clone(), accumulate=True)
     assert torch.equal(acc, dw + dw)
