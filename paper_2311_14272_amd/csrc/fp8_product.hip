@@ -9,6 +9,7 @@ static ProductArgs args_of(const crisp_fp8_mat& W, int64_t T, void* Y, int64_t l
     a.T = (int)T; a.S = (int)W.rows; a.K = (int)W.cols; a.kb = (int)((W.cols + FP8_BLOCK - 1) / FP8_BLOCK);
     a.w_tiles = W.kind == CRISP_FP8_TILES;
     a.y = Y; a.ldy = ldy; a.y_bf16 = y_type == CRISP_Y_BF16;
+    a.y_vec = ((uintptr_t)Y & 15) == 0 && ldy % (a.y_bf16 ? 8 : 4) == 0;
     if (ep) { a.scale = ep->scale; a.bias = ep->bias; a.residual = ep->residual; a.ldr = ep->ldr; a.relu = ep->relu; }
     return a;
 }

@@ -140,14 +140,11 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_split_kernel(ProductArgs a, in
     for (int e = threadIdx.x; e < MS * MT * 64; e += 64 * WAVES) {
         const int tile = e / 64, l = e % 64;
         f32x4 y = part[0][tile][l];
-#pragma unroll
+        // (four at a time: 64 registers let two workgroups of 16 waves run on a CU, 13 x 11008 x 4096 13.3 us against 14.4 with one)
+#pragma unroll 4
         for (int v = 1; v < WAVES; ++v) y += part[v][tile][l];
-        const int t = t0 + tile % MT * 16 + l % 16, s = s0 + tile / MT * 16 + l / 16 * 4;
-        if (t < a.T) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (s + j < a.S) store_y(a, t, s + j, y[j]);
-        }
+        float v[4] = {y[0], y[1], y[2], y[3]};
+        store_row<4, BF16>(a, t0 + tile % MT * 16 + l % 16, s0 + tile / MT * 16 + l / 16 * 4, v);
     }
 }
 

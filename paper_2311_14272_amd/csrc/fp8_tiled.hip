@@ -24,27 +24,6 @@ constexpr int XCDS = 8;
 __device__ __forceinline__ int x_swizzle(int r) { return (r >> 1) & 7; }                       // rows 16n .. 16n+15
 __device__ __forceinline__ int w_swizzle(int r) { return ((r >> 1) & 3) | ((r >> 2) & 4); }    // 8m+{0..7}, 8m+16+{0..7}
 
-// Sixteen consecutive results of row t from column s on.
-template <bool BF16>
-__device__ __forceinline__ void store_y16(const ProductArgs& a, int t, int s, const f32x16& v, bool plain) {
-    if (t >= a.T) return;
-    if (plain && s + 16 <= a.S) {
-        if constexpr (BF16) {
-            uint4* p = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.y) + t * a.ldy + s);
-            p[0] = make_uint4(to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7]));
-            p[1] = make_uint4(to_bf16x2(v[8], v[9]), to_bf16x2(v[10], v[11]), to_bf16x2(v[12], v[13]), to_bf16x2(v[14], v[15]));
-        } else {
-            f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + t * a.ldy + s);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) p[j] = f32x4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (s + j < a.S) store_y(a, t, s + j, v[j]);
-}
-
 // Waits until at most `left` of the wave's memory operations are outstanding, and for all its LDS reads.
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() {
@@ -320,12 +299,15 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         if (kg > 0) return;
     }
 
-    const bool plain = !a.scale && !a.bias && !a.residual && !a.relu && ((uintptr_t)a.y & 15) == 0 && a.ldy % (BF16 ? 8 : 4) == 0;
 #pragma unroll
     for (int r = 0; r < RS; ++r)
 #pragma unroll
-        for (int q = 0; q < RT; ++q)
-            store_y16<BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, acc[r][q], plain);
+        for (int q = 0; q < RT; ++q) {
+            float v[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = acc[r][q][j];
+            store_row<16, BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, v);
+        }
 }
 
 template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
