@@ -41,7 +41,7 @@ typedef struct {
 /* Values of a step that are read on the device when it runs: a captured step replays with the values of the moment. */
 typedef struct {
     float lr, grad_scale;
-    int32_t step;            /* >= 1                                                           */
+    int32_t step;            /* >= 1 (less counts as 1)                                        */
     int32_t skip;            /* not 0: the step changes nothing (gradients that overflowed)    */
 } crisp_adamw_live;
 
@@ -65,7 +65,8 @@ typedef struct {
  * stands for it, since the update would divide by eps alone in the next step.
  * A pruned position (mask bit not set) keeps its weight, its moments become zero, its gradient is not looked at; with
  * w_copy, the copy there has to hold the rounded weight already.
- * The tensors' buffers must not overlap.  tensors: host array of n_tensors elements (1 .. 2^20); everything is checked
+ * Without `live` a captured step replays with the lr, grad_scale and step that it was captured with.
+ * The tensors' buffers must not overlap, and a tensor comes once.  tensors: host array of n_tensors elements (1 .. 2^20); everything is checked
  * before anything is enqueued.  Errors: EINVAL, ESHAPE, EALIGN, EDEVICE.
  */
 CRISP_API crisp_status crisp_adamw_batch(int32_t n_tensors, const crisp_adamw_tensor *tensors,

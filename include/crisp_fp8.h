@@ -8,7 +8,8 @@
  * read operands that were quantised along the other direction.
  *
  * The conventions of crisp.h hold: status codes, arguments checked on the host before any device call, no allocation and
- * no synchronisation, work enqueued on `stream`.
+ * no synchronisation, work enqueued on `stream`.  What a call writes must not overlap what it reads, but for a residual that is
+ * Y itself.
  */
 #ifndef CRISP_FP8_H
 #define CRISP_FP8_H

@@ -95,6 +95,9 @@ class Batch:
             c.numel, c.row_len = t["w"].numel(), t["row_len"]
             c.w_type, c.g_type = _P[t["w"].dtype], _P[t["g"].dtype]
             c.moments, c.weight_decay = int(t["m_scale"] is not None), t["weight_decay"]
+        starts = [p for c in self.c if c.numel for p in (c.w, c.m, c.v, c.m_scale, c.v_scale, c.w_copy) if p]
+        if len(set(starts)) != len(starts):
+            raise ValueError("a tensor, or a buffer that a step writes, comes twice")
         self.device = tensors[0]["w"].device
 
 

@@ -1,7 +1,5 @@
 // One AdamW step over many tensors, and the bit mask of the hybrid pattern.  Both are bound by memory: every element is
 // read and written once, the arithmetic of the step (two roots' worth of it) hides behind that.
-#include <vector>
-
 #include "crisp_adamw.h"
 #include "crisp_internal.h"
 #include "fp8_common.h"
@@ -81,7 +79,7 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(AdamwArgs a) {
     AdamwScalars s = a.s;
     if (a.live) {
         if (a.live->skip) return;
-        s = adamw_scalars(a.live->lr, a.beta1, a.beta2, 0.0, a.live->grad_scale, a.live->step);
+        s = adamw_scalars(a.live->lr, a.beta1, a.beta2, 0.0, a.live->grad_scale, max(a.live->step, 1));
         s.eps = a.s.eps;
     }
     const float decay = (float)(1.0 - s.lr * (double)t.decay);

@@ -45,6 +45,12 @@ __device__ __forceinline__ void wait_loads() {
 // One object of LDS a stage: W's rows, X's rows, scales.  The compiler tells requests to LDS apart by the object that they write,
 // no more than eight of them, and follows few address steps from an object: every address here is an object and one offset.  Where
 // it cannot tell, a read of LDS waits for all requests.
+__device__ __forceinline__ void meet() {
+    asm volatile("" ::: "memory");           // (the compiler moves no access of LDS across; it emits nothing)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <int NS, int NT, int RS, int RT, int KG>
 struct Tiles {
     static constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
@@ -243,7 +249,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         const int step = step0 + k, b = step * KG + kg;                                                           \
         const int ahead = min(b + AHEAD * KG, a.kb - 1);                                                          \
         wait_loads<(AHEAD - 1) * PER>();                                                                          \
-        __builtin_amdgcn_s_barrier();                                                                             \
+        meet();                                                                                                   \
         if (KG > 1 && b >= a.kb) break;               /* the last step may have no block for the later groups */  \
         compute(st##here, [&](int tile) {                                                                         \
             _Pragma("unroll") for (int n = 0; n < PER; ++n)                                                       \

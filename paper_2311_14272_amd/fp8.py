@@ -137,9 +137,11 @@ def _input(x):
     return _here(x, "input"), _IN[x.dtype], rows, cols, x.stride(0) if rows > 1 else max(x.stride(0), cols)
 
 
-def _quant(x, mask, out, out_t, inp=None):
+def _quant(x, mask, out, out_t, inp=None, kind=None):
     p, t, rows, cols, ldx = inp or _input(x)
     _mats_here(out, out_t)
+    if kind is not None and ((out is not None and out.kind != kind) or (out_t is not None and out_t.kind != kind)):
+        raise ValueError("out has another kind of scales")
     if mask is not None:
         if mask.dtype != torch.int32 or not mask.is_contiguous() or mask.numel() < rows * (-(-cols // 32)):
             raise ValueError("mask: rows x ceil(cols/32) contiguous int32 words")
@@ -155,7 +157,7 @@ def quantize(x, kind=ROWS, mask=None, out=None) -> Fp8Mat:
     inp = _input(x)
     if out is None:
         out = _new(inp[2], inp[3], kind, x.device)
-    _quant(x, mask, out, None, inp)
+    _quant(x, mask, out, None, inp, kind)
     return out
 
 
@@ -166,7 +168,7 @@ def quantize_both(x, kind=ROWS, mask=None, out=None, out_t=None):
         out = _new(inp[2], inp[3], kind, x.device)
     if out_t is None:
         out_t = _new(inp[3], inp[2], kind, x.device)
-    _quant(x, mask, out, out_t, inp)
+    _quant(x, mask, out, out_t, inp, kind)
     return out, out_t
 
 

@@ -167,6 +167,24 @@ def test_steps_from_the_start(bits):
         assert torch.equal(a, b)
 
 
+def test_the_same_buffer_twice_is_refused():
+    w, g = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
+    a, b = adamw.tensor(w, g, **adamw.alloc_moments(64)), adamw.tensor(w, g, **adamw.alloc_moments(64))
+    for two in ([a, a], [a, b], [adamw.tensor(w, g, m := torch.zeros(64, device="cuda"), m)]):
+        with pytest.raises(ValueError):
+            adamw.make_batch(two)
+    adamw.make_batch([a, adamw.tensor(torch.zeros(64, device="cuda"), g, **adamw.alloc_moments(64))])     # (a gradient may be shared)
+
+
+def test_live_step_below_one_counts_as_one():
+    rng = np.random.default_rng(12)
+    c = Case(rng, 500, True, True, 32)
+    h = dict(HYPER, lr=float(np.float32(3e-3)), step=1)
+    want = c.plain(h)
+    adamw.step(adamw.make_batch([c.tensor()]), beta1=0.9, beta2=0.999, eps=1e-8, live=adamw.live(3e-3, 0, 0.5))
+    c.check(want)
+
+
 def test_extremes():
     """Zero gradients and moments move nothing but the decay; infinities and NaN stay in their element (32 bits) or their block
     of 128 (8 bits); a second moment far below its block's largest keeps the smallest code instead of zero."""

@@ -229,6 +229,26 @@ def test_linear_is_quantize_and_product(shape, dtype):
                                fp8.product(x8, weights, out_dtype=torch.float32, bias=bias))
 
 
+def test_refusals_that_the_binding_makes():
+    x = torch.randn((8, 256), device="cuda")
+    x8, t8 = fp8.quantize(x), fp8.quantize(x, fp8.TILES)
+    for bad in (lambda: fp8.quantize(x, fp8.ROWS, out=t8), lambda: fp8.quantize(x.t()), lambda: fp8.quantize(x[:0]),
+                lambda: fp8.quantize(x.half()), lambda: fp8.quantize(x.cpu()), lambda: fp8.linear(x[:, :128], t8),
+                lambda: fp8.linear(x, t8, out=torch.empty((8, 9), device="cuda")), lambda: fp8.linear(x, t8, bias=torch.zeros(9, device="cuda")),
+                lambda: fp8.linear(x, t8, bias=torch.zeros(8, device="cuda"), ep=crisp.epilogue()),
+                lambda: fp8.quantize(x, mask=torch.zeros(63, dtype=torch.int32, device="cuda")),
+                lambda: fp8.Fp8Mat(x8.q, x8.scale, 8, 257, fp8.ROWS), lambda: fp8.Fp8Mat(x8.q, x8.scale.t(), 8, 256, fp8.ROWS),
+                lambda: fp8.linear_backward(x, None, None, dw=x), lambda: fp8.linear_backward(x, x8, None, accumulate=True)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: fp8.product(t8, x8),                                        # X with scales of tiles
+                lambda: fp8.quantize(x[:1].expand(8, 256)),                         # rows that overlap
+                lambda: fp8.product(x8, fp8.quantize(x[:, :128].contiguous())),     # another number of columns
+                lambda: fp8.quantize(x, out=fp8.alloc_mat(9, 256)), lambda: fp8.linear_backward(x, None, None)):
+        with pytest.raises(crisp.CrispError):
+            bad()
+
+
 def test_rows_far_apart_in_many():
     """Row strides of 2^24 and more: more rows than the kernels without staging are chosen for by their number."""
     ld, K = 1 << 24, 200
