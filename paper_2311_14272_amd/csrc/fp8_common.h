@@ -64,28 +64,86 @@ __device__ __forceinline__ uint32_t to_bf16x2(float a, float b) {
 }
 __device__ __forceinline__ uint16_t to_bf16(float a) { return __builtin_bit_cast(uint16_t, (__bf16)a); }
 
-// Eight elements of a row from column c on; what lies at or behind `cols` counts as zero.  vec: the address is a multiple of
-// 16 bytes wherever c is a multiple of 8.
-template <bool BF16>
-__device__ __forceinline__ void load8(const void* X, int64_t at, int64_t left, bool vec, float (&x)[8]) {
-    if (vec && left >= 8) {
-        if constexpr (BF16) {
-            from_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + at), x);
+// Vectors at any address: the hardware takes them in one request also where they are not aligned.
+typedef uint32_t loose_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t loose_u32x4 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float loose_f32x4 __attribute__((ext_vector_type(4), aligned(2)));
+
+// C (four or eight) elements of a row as they lie in memory, from column c on; columns at or behind `cols` are zeros.
+template <bool BF16, int C>
+struct Elements {
+    static constexpr int WORDS = BF16 ? C / 2 : C;
+    uint32_t w[WORDS];
+
+    // cols >= C: of the row's last C elements where the wanted ones end behind it, so that every lane makes the same request and
+    // those of several rows are under way together.  settle() then moves them to their places.
+    __device__ __forceinline__ void request(const void* X, int64_t row_at, int64_t c, int64_t cols) {
+        const int64_t at = row_at + (c < cols - C ? c : cols - C);
+        const uint8_t* p = static_cast<const uint8_t*>(X) + at * (BF16 ? 2 : 4);
+        if constexpr (WORDS == 2) {
+            const loose_u32x2 v = *reinterpret_cast<const loose_u32x2*>(p);
+            w[0] = v[0]; w[1] = v[1];
         } else {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at);
-            const f32x4 b = *reinterpret_cast<const f32x4*>(static_cast<const float*>(X) + at + 4);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { x[j] = a[j]; x[4 + j] = b[j]; }
+            for (int k = 0; k < WORDS; k += 4) {
+                const loose_u32x4 v = *reinterpret_cast<const loose_u32x4*>(p + k * 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[k + j] = v[j];
+            }
         }
-        return;
     }
+
+    __device__ __forceinline__ void settle(int64_t c, int64_t cols) {
+        int64_t ahead = c - (cols - C);      // elements before the wanted ones
+        for (ahead = ahead < C ? ahead : C; ahead > 0; --ahead) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[j] = 0.0f;
-        if (j < left) {
-            if constexpr (BF16) x[j] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(X)[at + j] << 16);
-            else x[j] = static_cast<const float*>(X)[at + j];
+            for (int j = 0; j < WORDS; ++j) {
+                const uint32_t next = j + 1 < WORDS ? w[j + 1] : 0;
+                w[j] = BF16 ? w[j] >> 16 | next << 16 : next;
+            }
         }
+    }
+
+    // cols < C: one by one.
+    __device__ __forceinline__ void gather(const void* X, int64_t row_at, int64_t c, int64_t cols) {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < C - 1; ++j)
+            if (c + j < cols) {
+                if constexpr (BF16) w[j / 2] |= (uint32_t)static_cast<const uint16_t*>(X)[row_at + c + j] << (j % 2 * 16);
+                else w[j] = static_cast<const uint32_t*>(X)[row_at + c + j];
+            }
+    }
+
+    // bit j of `bits`: whether element j stays, else zero
+    __device__ __forceinline__ void keep(uint32_t bits) {
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) {
+            if constexpr (BF16) w[j] &= ((bits >> (2 * j) & 1) ? 0xffffu : 0u) | ((bits >> (2 * j + 1) & 1) ? 0xffff0000u : 0u);
+            else w[j] = bits >> j & 1 ? w[j] : 0u;
+        }
+    }
+
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (BF16) return __uint_as_float(j % 2 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+        else return __uint_as_float(w[j]);
+    }
+};
+
+// Elements c, c + 1, ... of N rows, all requested before any is used; row_at: where a row starts.
+template <int N, bool BF16, int C, typename At>
+__device__ __forceinline__ void read_rows(Elements<BF16, C> (&x)[N], const void* X, int64_t c, int64_t cols, At row_at) {
+    if (cols >= C) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i].request(X, row_at(i), c, cols);
+        if (c > cols - C) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i].settle(c, cols);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i].gather(X, row_at(i), c, cols);
     }
 }
 

@@ -22,9 +22,4 @@ bool fp8_takes_raw(int64_t T, int64_t K);
 hipError_t launch_fp8_raw(const void* X, int in_type, int64_t T, int64_t ldx, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
                           const crisp_epilogue* ep, hipStream_t st);
 
-// Whether every eight elements of a row, from a multiple of eight on, are at a multiple of 16 bytes.
-inline bool fp8_whole_vectors(const void* X, int in_type, int64_t ldx) {
-    return ((uintptr_t)X & 15) == 0 && (ldx * (in_type == CRISP_IN_BF16 ? 2 : 4)) % 16 == 0;
-}
-
 }  // namespace crisp

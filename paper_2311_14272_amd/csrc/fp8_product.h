@@ -24,10 +24,9 @@ struct ProductArgs {
     const float *scale, *bias;
     const void* residual;
     int relu, y_bf16;
-    int y_vec;                          // rows of Y start at multiples of 16 bytes
     const void* raw;                    // X before it is quantised (T x K of row stride ldraw), where the kernel does that; else NULL
     int64_t ldraw;
-    int raw_bf16, raw_vec, K;
+    int raw_bf16, K;
 };
 
 // Blocks of X that a workgroup of fp8_split_kernel quantises for itself.  Its 512 or 1024 threads take 32 or 64 of them in
@@ -87,18 +86,18 @@ __device__ __forceinline__ void store_row(const ProductArgs& a, int64_t t, int s
         for (int j = 0; j < N; ++j) v[j] = fmaxf(v[j], 0.0f);
     }
     const int64_t at = t * a.ldy + s;
-    if (a.y_vec && s + N <= a.S) {           // (s is a multiple of N)
+    if (s + N <= a.S) {
         if constexpr (BF16) {
             uint16_t* p = static_cast<uint16_t*>(a.y) + at;
 #pragma unroll
             for (int j = 0; j < N; j += 8) {
-                if constexpr (N == 4) *reinterpret_cast<uint2*>(p) = make_uint2(to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]));
-                else *reinterpret_cast<uint4*>(p + j) = make_uint4(to_bf16x2(v[j], v[j + 1]), to_bf16x2(v[j + 2], v[j + 3]),
-                                                                   to_bf16x2(v[j + 4], v[j + 5]), to_bf16x2(v[j + 6], v[j + 7]));
+                if constexpr (N == 4) *reinterpret_cast<loose_u32x2*>(p) = loose_u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
+                else *reinterpret_cast<loose_u32x4*>(p + j) = loose_u32x4{to_bf16x2(v[j], v[j + 1]), to_bf16x2(v[j + 2], v[j + 3]),
+                                                                   to_bf16x2(v[j + 4], v[j + 5]), to_bf16x2(v[j + 6], v[j + 7])};
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < N; j += 4) *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+            for (int j = 0; j < N; j += 4) *reinterpret_cast<loose_f32x4*>(static_cast<float*>(a.y) + at + j) = loose_f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
         }
         return;
     }

@@ -9,7 +9,6 @@ static ProductArgs args_of(const crisp_fp8_mat& W, int64_t T, void* Y, int64_t l
     a.T = (int)T; a.S = (int)W.rows; a.K = (int)W.cols; a.kb = (int)((W.cols + FP8_BLOCK - 1) / FP8_BLOCK);
     a.w_tiles = W.kind == CRISP_FP8_TILES;
     a.y = Y; a.ldy = ldy; a.y_bf16 = y_type == CRISP_Y_BF16;
-    a.y_vec = ((uintptr_t)Y & 15) == 0 && ldy % (a.y_bf16 ? 8 : 4) == 0;
     if (ep) { a.scale = ep->scale; a.bias = ep->bias; a.residual = ep->residual; a.ldr = ep->ldr; a.relu = ep->relu; }
     return a;
 }
@@ -46,7 +45,6 @@ hipError_t launch_fp8_raw(const void* X, int in_type, int64_t T, int64_t ldx, co
                           const crisp_epilogue* ep, hipStream_t st) {
     ProductArgs a = args_of(W, T, Y, ldy, y_type, ep);
     a.raw = X; a.ldraw = ldx; a.raw_bf16 = in_type == CRISP_IN_BF16;
-    a.raw_vec = fp8_whole_vectors(X, in_type, ldx);
     return launch_fp8_split(a, st);
 }
 

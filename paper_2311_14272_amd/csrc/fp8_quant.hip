@@ -8,7 +8,7 @@ namespace crisp {
 // ROWS, one direction, no mask: 16 lanes take a block of 128 columns, a workgroup 16 consecutive blocks of the matrix in
 // row order.
 template <bool BF16>
-__global__ __launch_bounds__(256) void fp8_rows_kernel(const void* __restrict__ X, int64_t rows, int cols, int64_t ldx, bool vec,
+__global__ __launch_bounds__(256) void fp8_rows_kernel(const void* __restrict__ X, int64_t rows, int cols, int64_t ldx,
                                                        uint8_t* __restrict__ q, int64_t ld, float* __restrict__ scale, int64_t lds) {
     const int kb = (cols + FP8_BLOCK - 1) / FP8_BLOCK;
     const int64_t id = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
@@ -16,54 +16,27 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const void* __restrict__ 
     const int b = (int)(id - r * kb), lane = threadIdx.x % 16;
     if (r >= rows) return;      // all 16 lanes of a group leave together
     const int c = b * FP8_BLOCK + lane * 8;
+    Elements<BF16, 8> in[1];
+    read_rows(in, X, c, cols, [&](int) { return r * ldx; });
     float x[8], s;
-    load8<BF16>(X, r * ldx + c, cols - c, vec, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = in[0][j];
     *reinterpret_cast<uint2*>(q + r * ld + c) = quantize_block(x, s);
     if (lane == 0) scale[b * lds + r] = s;
 }
 
-// C elements of a row from column c on; what lies at or behind `cols` counts as zero.  vec: as in load8.
-template <bool BF16, int C>
-__device__ __forceinline__ void load_some(const void* X, int64_t at, int64_t left, bool vec, float (&x)[C]) {
-    if constexpr (C == 8) {
-        load8<BF16>(X, at, left, vec, x);
-    } else {
-        typedef uint32_t words __attribute__((ext_vector_type(BF16 ? C / 2 : C)));
-        if (vec && left >= C) {
-            if constexpr (BF16) {
-                const words v = *reinterpret_cast<const words*>(static_cast<const uint16_t*>(X) + at);
-#pragma unroll
-                for (int j = 0; j < C / 2; ++j) { x[2 * j] = __uint_as_float(v[j] << 16); x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u); }
-            } else {
-                const words v = *reinterpret_cast<const words*>(static_cast<const float*>(X) + at);
-#pragma unroll
-                for (int j = 0; j < C; ++j) x[j] = __uint_as_float(v[j]);
-            }
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            x[j] = 0.0f;
-            if (j < left) {
-                if constexpr (BF16) x[j] = __uint_as_float((uint32_t)static_cast<const uint16_t*>(X)[at + j] << 16);
-                else x[j] = static_cast<const float*>(X)[at + j];
-            }
-        }
-    }
-}
-
-// A 128 x 128 tile per workgroup, for everything else.  Thread (g, l): rows 8g .. 8g+7, columns Cl .. Cl+C-1, held in registers.
-// Largest magnitudes meet in LDS, where one thread each makes the scale of a row or column.  The transpose is eight bytes per
-// column and thread, gathered in LDS so that it leaves in whole rows.
-// C = 8 reads 16 bytes of bf16 at a time: 8192 x 4096 in both directions 33.0 us, with C = 4 34.8.  C = 4 has the shorter way from a
-// tile's first load to its last store, the time where CUs have a tile or two: 500 x 512 5.4 us against 7.4, 2048 x 2048 6.6
-// against 7.4 (C = 2: 5.4 and 6.9).
-template <bool BF16, int C>
-__global__ __launch_bounds__(2048 / C) void fp8_tile_kernel(const void* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx, bool vec,
-                                                            const uint32_t* __restrict__ mask, int kind, int tiles_c,
-                                                            uint8_t* __restrict__ q, int64_t ld, float* __restrict__ scale, int64_t lds,
-                                                            uint8_t* __restrict__ qt, int64_t ldt, float* __restrict__ scale_t,
-                                                            int64_t ldst) {
+// A 128 x 128 tile per workgroup, for everything else.  Thread (g, l): rows 8g .. 8g+7, columns 4l .. 4l+3, held in registers as
+// they were read.  Largest magnitudes meet in LDS, where one thread each makes the scale of a row or column.  The transpose is
+// eight bytes per column and thread, gathered in LDS so that it leaves in whole rows.
+// bf16 in both directions: 8192 x 4096 26.6 us (128 MiB, 5.0 TB/s), 2048 x 2048 6.3, 500 x 512 4.7; with eight columns a thread, half as
+// many of them, 26.1, 6.9 and 5.4.  With conditions around the reads, each waiting for the one before, 34.8, 6.6 and 5.4.
+constexpr int C = 4;
+template <bool BF16>
+__global__ __launch_bounds__(512) void fp8_tile_kernel(const void* __restrict__ X, int64_t rows, int64_t cols, int64_t ldx,
+                                                       const uint32_t* __restrict__ mask, int kind, int tiles_c,
+                                                       uint8_t* __restrict__ q, int64_t ld, float* __restrict__ scale, int64_t lds,
+                                                       uint8_t* __restrict__ qt, int64_t ldt, float* __restrict__ scale_t,
+                                                       int64_t ldst) {
     constexpr int L = FP8_BLOCK / C, THREADS = 16 * L, WAVES = THREADS / 64;
     __shared__ uint32_t row_top[FP8_BLOCK], col_top[WAVES][FP8_BLOCK];
     __shared__ float row_inv[FP8_BLOCK], col_inv[FP8_BLOCK];
@@ -72,17 +45,22 @@ __global__ __launch_bounds__(2048 / C) void fp8_tile_kernel(const void* __restri
     const int64_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
     const int tid = threadIdx.x, l = tid % L, g = tid / L, wave = tid / 64, lane = tid % 64;
     const int64_t c = tc * FP8_BLOCK + l * C, r0 = tr * FP8_BLOCK + g * 8;
-    float x[8][C];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) load_some<BF16, C>(X, (r0 + i) * ldx + c, r0 + i < rows ? cols - c : 0, vec, x[i]);
+    auto row = [&](int i) { return r0 + i < rows ? r0 + i : rows - 1; };      // (rows behind the last one repeat it, and are zeros below)
+    uint32_t bits[8];
     if (mask) {
-        const int64_t words = (cols + 31) / 32;
+        const int64_t words = (cols + 31) / 32, word = c < cols ? c / 32 : 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = r0 + i < rows && c < cols ? mask[(r0 + i) * words + c / 32] >> (c % 32) : 0u;
+        for (int i = 0; i < 8; ++i) bits[i] = mask[row(i) * words + word];
+    }
+    Elements<BF16, C> x[8];
+    read_rows(x, X, c, cols, [&](int i) { return row(i) * ldx; });
+    if (mask) {
 #pragma unroll
-            for (int j = 0; j < C; ++j) x[i][j] = (bits >> j) & 1u ? x[i][j] : 0.0f;
-        }
+        for (int i = 0; i < 8; ++i) x[i].keep(bits[i] >> (c % 32));
+    }
+    if (r0 + 8 > rows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i].keep(r0 + i < rows ? ~0u : 0u);
     }
     const bool tiles = kind == CRISP_FP8_TILES;
     uint32_t top[C];
@@ -98,13 +76,12 @@ __global__ __launch_bounds__(2048 / C) void fp8_tile_kernel(const void* __restri
             top[j] = umax(top[j], b);
         }
         t = max16(t);
-        if constexpr (L > 16) t = umax(t, (uint32_t)__shfl_xor((int)t, 16));
+        t = umax(t, (uint32_t)__shfl_xor((int)t, 16));
         if (l == i) row_top[g * 8 + i] = t;
     }
     if (!tiles && qt) {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-            if constexpr (L < 32) top[j] = umax(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
             top[j] = umax(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
             if (lane < L) col_top[wave][l * C + j] = top[j];
         }
@@ -144,14 +121,8 @@ __global__ __launch_bounds__(2048 / C) void fp8_tile_kernel(const void* __restri
 #pragma unroll
             for (int j = 0; j < C; ++j) y[j] = x[i][j] * inv;
             if (r0 + i < rows) {
-                uint8_t* to = q + (r0 + i) * ld + c;
-                if constexpr (C == 8) {
-                    *reinterpret_cast<uint2*>(to) = to_fp8x8(y);
-                } else {
-                    static_assert(C == 4, "four bytes");
-                    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-                    *reinterpret_cast<int*>(to) = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-                }
+                const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+                *reinterpret_cast<int*>(q + (r0 + i) * ld + c) = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
             }
         }
     }
@@ -173,26 +144,21 @@ __global__ __launch_bounds__(2048 / C) void fp8_tile_kernel(const void* __restri
     }
 }
 
-constexpr unsigned FEW_TILES = 512;      // two a CU
-
 hipError_t launch_fp8_quant(const void* X, int in_type, int64_t rows, int64_t cols, int64_t ldx, const uint32_t* mask,
                             const crisp_fp8_mat* Q, const crisp_fp8_mat* Qt, hipStream_t st) {
     const bool bf16 = in_type == CRISP_IN_BF16;
-    const bool vec = fp8_whole_vectors(X, in_type, ldx);
     const int64_t rb = (rows + FP8_BLOCK - 1) / FP8_BLOCK, cb = (cols + FP8_BLOCK - 1) / FP8_BLOCK;
     const int kind = Q ? Q->kind : Qt->kind;
     if (kind == CRISP_FP8_ROWS && !Qt && !mask) {
         const unsigned grid = (unsigned)((rows * cb + 15) / 16);
-        if (bf16) fp8_rows_kernel<true><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, vec, Q->q, Q->ld, Q->scale, Q->lds);
-        else fp8_rows_kernel<false><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, vec, Q->q, Q->ld, Q->scale, Q->lds);
+        if (bf16) fp8_rows_kernel<true><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, Q->q, Q->ld, Q->scale, Q->lds);
+        else fp8_rows_kernel<false><<<grid, 256, 0, st>>>(X, rows, (int)cols, ldx, Q->q, Q->ld, Q->scale, Q->lds);
         return hipGetLastError();
     }
     const crisp_fp8_mat none = {};
     const crisp_fp8_mat &a = Q ? *Q : none, &b = Qt ? *Qt : none;
-    const unsigned grid = (unsigned)(rb * cb);
-    const bool few = grid <= FEW_TILES;
-    auto kernel = few ? (bf16 ? fp8_tile_kernel<true, 4> : fp8_tile_kernel<false, 4>) : (bf16 ? fp8_tile_kernel<true, 8> : fp8_tile_kernel<false, 8>);
-    kernel<<<grid, few ? 512 : 256, 0, st>>>(X, rows, cols, ldx, vec, mask, kind, (int)cb, a.q, a.ld, a.scale, a.lds, b.q, b.ld, b.scale, b.lds);
+    auto kernel = bf16 ? fp8_tile_kernel<true> : fp8_tile_kernel<false>;
+    kernel<<<(unsigned)(rb * cb), 512, 0, st>>>(X, rows, cols, ldx, mask, kind, (int)cb, a.q, a.ld, a.scale, a.lds, b.q, b.ld, b.scale, b.lds);
     return hipGetLastError();
 }
 

@@ -84,8 +84,15 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_split_kernel(ProductArgs a, in
             if (e < blocks) {
                 const int t = e / a.kb, c = (e - t * a.kb) * 128 + threadIdx.x % 16 * 8;
                 float v[8], scale;
-                if (a.raw_bf16) load8<true>(a.raw, t * a.ldraw + c, a.K - c, a.raw_vec, v);
-                else load8<false>(a.raw, t * a.ldraw + c, a.K - c, a.raw_vec, v);
+                auto own = [&](auto in) {
+                    read_rows(in.x, a.raw, c, a.K, [&](int) { return t * a.ldraw; });
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = in.x[0][j];
+                };
+                struct Half { Elements<true, 8> x[1]; };
+                struct Whole { Elements<false, 8> x[1]; };
+                if (a.raw_bf16) own(Half());
+                else own(Whole());
                 *reinterpret_cast<uint2*>(own_q + e * 128 + threadIdx.x % 16 * 8) = quantize_block(v, scale);
                 if (threadIdx.x % 16 == 0) own_s[e] = scale;
             }

@@ -111,6 +111,46 @@ def test_quantize_extremes(kind):
         assert _same(_np(a.q), q) and _same(_np(a.scale), s) and np.isfinite(_np(a.q)).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_quantize_row_ends(dtype):
+    """Rows that end anywhere in a vector, from any address, among NaN: the matrix, its transpose and the layer that quantises
+    for itself see the row's own elements only."""
+    rng = np.random.default_rng(21)
+    for C in [*range(1, 18), *range(121, 137), 260, 389]:
+        R, gap, offset = 3 + C % 7, int(rng.integers(1, 9)), int(rng.integers(0, 9))
+        x = torch.from_numpy(rng.normal(size=(R, C)).astype(np.float32)).to(dtype)
+        store = torch.full((R * (C + gap) + offset,), float("nan"), dtype=dtype, device="cuda")
+        view = store[offset:].view(R, C + gap)[:, :C]
+        view.copy_(x)
+        xh, keep = x.float().numpy(), rng.random((R, C)) < 0.5
+        mask = torch.from_numpy(U.bits_of(keep)).cuda()
+        for m, k in ((None, None), (mask, keep)):
+            a, b = fp8.quantize_both(view, mask=m)
+            one = fp8.quantize(view, mask=m)
+            q, s = U.quant(xh, False, k)
+            qt, st = U.quant(np.ascontiguousarray((xh if k is None else np.where(k, xh, 0)).T), False)
+            for got in (a, one):
+                assert _same(_np(got.q), q) and _same(_np(got.scale), s), (C, gap, offset)
+            assert _same(_np(b.q), qt) and _same(_np(b.scale), st), (C, gap, offset)
+        W = fp8.quantize(torch.from_numpy(rng.normal(size=(20, C)).astype(np.float32)).cuda())
+        assert torch.equal(fp8.linear(view, W), fp8.product(fp8.quantize(view), W)), (C, gap, offset)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(5, 37, 130), (40, 37, 130), (90, 203, 260), (130, 259, 128)], ids=str)
+def test_product_into_any_place(shape, dtype):
+    """Y at any address and row stride gets the same bits, and nothing around it changes."""
+    T, S, K = shape
+    X, W, _, _ = _pair(S, T, S, K, True)
+    want = fp8.product(X, W, out_dtype=dtype)
+    for offset, gap in ((1, 0), (3, 1), (8, 2), (5, 8 - S % 8), (0, 7)):
+        store = torch.full((T * (S + gap) + offset + 9,), -3.0, dtype=dtype, device="cuda")
+        rows = store[offset:offset + T * (S + gap)].view(T, S + gap)
+        fp8.product(X, W, out=rows[:, :S])
+        assert torch.equal(rows[:, :S], want)
+        assert (rows[:, S:] == -3).all() and (store[:offset] == -3).all() and (store[offset + T * (S + gap):] == -3).all()
+
+
 # ---- products ---------------------------------------------------------------------------------------------------
 
 def _pair(seed, T, S, K, w_tiles):
