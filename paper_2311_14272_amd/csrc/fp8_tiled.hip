@@ -32,7 +32,7 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // NS x NT waves, each RS x RT tiles of 32 x 32; STAGES blocks in LDS, all but one of them on their way.  BF16: the result's
-// type, and with it the instruction.  TILES: W has a scale for 128 x 128, one for all of a wave's rows.
+// type, and with it the instruction.  TILES: W has a scale for 128 x 128.
 //
 // KG: groups of waves that take the blocks in turn, for sizes whose tiles leave most CUs with one workgroup or none: a step then
 // costs its latencies (a barrier, LDS reads, two dependent matrix instructions: 0.5 us measured), whatever it computes.  Their
@@ -145,6 +145,8 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
     };
 
     const int xscale = W + X + 4 * (kg * SC + BS + wt * RT * 32 + i), wscales = W + X + 4 * (kg * SC + ws * RS * 32 + (TILES ? 0 : 16 * h));
+    // one scale for all of a wave's W rows (otherwise one for 32: those never lie in two blocks)
+    constexpr bool ONE = TILES && 128 % (RS * 32) == 0;
     auto compute = [&](const uint8_t* st, auto part) {
         i32x4 xv[RT][4], wv[4];
         float f[RT];
@@ -159,7 +161,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
             for (int c = 0; c < 4; ++c) xv[q][c] = *reinterpret_cast<const i32x4*>(st + (xr[c] + q * 4096));
 #pragma unroll
         for (int q = 0; q < RT; ++q) f[q] = *reinterpret_cast<const float*>(st + (xscale + q * 128));
-        const float wscale = TILES ? *reinterpret_cast<const float*>(st + wscales) : 0.0f;
+        float wscale = TILES ? *reinterpret_cast<const float*>(st + wscales) : 0.0f;
         __builtin_amdgcn_sched_barrier(0);
         f32x4 wsv[4];
         const f32x16 zero = {};
@@ -182,7 +184,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
                             __builtin_amdgcn_sched_barrier(0);
                         }
                     }
-                    if (TILES && k == 0) {
+                    if (ONE && k == 0) {
 #pragma unroll
                         for (int e = 0; e < RT; ++e) f[e] *= wscale;
                     }
@@ -195,8 +197,10 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
 #pragma unroll
                         for (int c = 0; c < 4; ++c) wsv[c] = *reinterpret_cast<const f32x4*>(st + (wscales + r * 128 + 16 * c));
                     }
+                    const float both = TILES && !ONE ? f[q] * wscale : f[q];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
+                    for (int j = 0; j < 16; ++j) acc[r][q][j] = __builtin_fmaf(p[(k - 1) % 2][j], TILES ? both : f[q] * wsv[j / 4][j % 4], acc[r][q][j]);
+                    if (TILES && !ONE && q == RT - 1 && r + 1 < RS) wscale = *reinterpret_cast<const float*>(st + (wscales + (r + 1) * 128));
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -220,19 +224,20 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
                             p[r % 2][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wa, xw[q][u], u ? p[r % 2][q] : zero, 0, 0, 0);
                         }
                         if (u % 2 == 1 && r + 1 < RS) wv[u / 2] = *reinterpret_cast<const i32x4*>(st + (wr[u / 2] + (r + 1) * 4096));
-                        if (u == 1 && r == 0 && TILES) {
+                        if (u == 1 && r == 0 && ONE) {
 #pragma unroll
                             for (int e = 0; e < RT; ++e) f[e] *= wscale;
                         }
-                        if (u % (8 / RT) == 8 / RT - 1) part(r * RT + u / (8 / RT));
+                        if (u % (8 / RT) == 8 / RT - 1 && u / (8 / RT) < RT) part(r * RT + u / (8 / RT));
                     }
                     if (r > 0) {
 #pragma unroll
                         for (int q = 0; q < RT; ++q)
 #pragma unroll
                             for (int j = 2 * u; j < 2 * u + 2; ++j)
-                                acc[r - 1][q][j] = __builtin_fmaf(p[(r - 1) % 2][q][j], TILES ? f[q] : f[q] * wsv[j / 4][j % 4], acc[r - 1][q][j]);
+                                acc[r - 1][q][j] = __builtin_fmaf(p[(r - 1) % 2][q][j], ONE ? f[q] : TILES ? f[q] * wscale : f[q] * wsv[j / 4][j % 4], acc[r - 1][q][j]);
                     }
+                    if (TILES && !ONE && u == 7 && r > 0 && r < RS) wscale = *reinterpret_cast<const float*>(st + (wscales + r * 128));
                     if (r < RS) __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -340,25 +345,34 @@ static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT * KG, 0, st>>>(a, ts, tt);
 }
 
-// The tile: the fewest rounds of 256 workgroups (each takes a CU's LDS) times what a step of a block takes, in microseconds as
-// measured with S = K = 4096.  Results in fp32 have twice the matrix work and the widening, and no registers left for 256 x 256.
-// W with a scale for each row costs registers too (256 x 256 spills).
+// The tile: the fewest rounds of 256 workgroups (each takes a CU's LDS), each the time of its blocks and of a first request and a
+// last store that nothing hides, in microseconds as measured with 16 x 16 tiles and K = 1024 and 4096.  Results in fp32 have
+// twice the matrix work and the widening, and registers for no more than 128 x 256; W with a scale for each row costs some too
+// (256 x 256 spills).  On 32 sizes of 64 x 256 x 128 to 8192 x 5120 x 256 the rule's choice takes 1 % longer than the best of all, in
+// the geometric mean, 11 % at the most.
 //
-//   T of S = K = 4096, bf16, us:   256    512   1024   2048   4096   8192
-//   64 x 64, two groups           10.3     24     46     89    158    294
-//   128 x 64, two groups            17   14.6     34     66    117    220
-//   128 x 128                                   22.2     47     94    175
-//   128 x 256                                     32   36.5     74    148
-//   256 x 256                                            53     64    119
+//   us, K = 4096, 256 tiles:   bf16, W tiles   bf16, W rows   fp32
+//   64 x 64, two groups           11.7            11.8        18.1
+//   128 x 64, two groups          15.9            18.0        27.9
+//   128 x 128                     24.3            28.6        48.6
+//   192 x 128                     31.6            37.4        63.9
+//   128 x 256                     38.9            43.7        85.2
+//   192 x 256                     51.5            58.4
+//   256 x 256                     64.6
+enum { SHAPES = 7 };
 static int tile_shape(const ProductArgs& a) {
-    static const struct { int bs, bt; float step[2]; } shapes[] = {         // [BF16]
-        {64, 64, {0.49f, 0.32f}}, {128, 64, {0.82f, 0.46f}}, {128, 128, {1.45f, 0.69f}}, {128, 256, {2.3f, 1.14f}}, {256, 256, {0.0f, 2.0f}}};
+    static const struct { int bs, bt; float step[3], rest[3]; } shapes[SHAPES] = {         // fp32; bf16: W tiles, W rows; 0: none
+        {64, 64, {0.42f, 0.22f, 0.23f}, {4.6f, 4.6f, 4.5f}},     {128, 64, {0.65f, 0.34f, 0.41f}, {7.0f, 5.0f, 4.8f}},
+        {128, 128, {1.20f, 0.59f, 0.73f}, {10.3f, 5.4f, 5.4f}},  {192, 128, {1.59f, 0.78f, 0.96f}, {13.0f, 6.5f, 6.7f}},
+        {128, 256, {2.19f, 0.96f, 1.12f}, {15.2f, 8.1f, 8.0f}},  {192, 256, {0.0f, 1.33f, 1.54f}, {0.0f, 9.1f, 9.1f}},
+        {256, 256, {0.0f, 1.68f, 0.0f}, {0.0f, 10.9f, 0.0f}}};
+    const int type = !a.y_bf16 ? 0 : a.w_tiles ? 1 : 2;
     int best = 0;
     float least = 0.0f;
-    for (int k = 0; k < 5; ++k) {
-        if (k == 4 && !(a.y_bf16 && a.w_tiles)) continue;
+    for (int k = 0; k < SHAPES; ++k) {
+        if (shapes[k].step[type] == 0.0f) continue;
         const int64_t n = (int64_t)((a.S + shapes[k].bs - 1) / shapes[k].bs) * ((a.T + shapes[k].bt - 1) / shapes[k].bt);
-        const float cost = (float)((n + 255) / 256) * shapes[k].step[a.y_bf16];
+        const float cost = (float)((n + 255) / 256) * ((float)a.kb * shapes[k].step[type] + shapes[k].rest[type]);
         if (k == 0 || cost < least) { best = k; least = cost; }
     }
     return best;
@@ -383,8 +397,11 @@ hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
         case 3: launch_tiles<2, 2, 2, 1, 3, 2, true>(a, st); break;
         case 4: launch_tiles<2, 4, 2, 1, 4, 1, false>(a, st); break;
         case 5: launch_tiles<2, 4, 2, 1, 4, 1, true>(a, st); break;
-        case 6: launch_tiles<2, 4, 2, 2, 3, 1, false>(a, st); break;
-        case 7: launch_tiles<2, 4, 2, 2, 3, 1, true>(a, st); break;
+        case 6: launch_tiles<2, 4, 3, 1, 3, 1, false>(a, st); break;
+        case 7: launch_tiles<2, 4, 3, 1, 3, 1, true>(a, st); break;
+        case 8: launch_tiles<2, 4, 2, 2, 3, 1, false>(a, st); break;
+        case 9: launch_tiles<2, 4, 2, 2, 3, 1, true>(a, st); break;
+        case 11: launch_tiles<2, 4, 3, 2, 2, 1, true>(a, st); break;
         default: launch_tiles<2, 4, 4, 2, 2, 1, true>(a, st); break;
     }
     return hipGetLastError();
