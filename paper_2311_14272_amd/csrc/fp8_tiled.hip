@@ -31,6 +31,31 @@ __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | 0 << 8 | (LEFT >> 4) << 14);
 }
 
+// A wave's 32 x 32 results, register j of lane (i, h) row t0 + i and column s0 + 16h + j, through the epilogue and out.  They change
+// lanes in LDS (4 KiB of the wave's own) so that a request writes whole rows of the tile: as 16 bytes here and there they left at
+// 2 TB/s.
+template <bool BF16>
+__device__ __forceinline__ void store_tile(const ProductArgs& a, int t0, int s0, const f32x16& sums, float* own, int lane) {
+    constexpr int N = BF16 ? 8 : 4, LANES = 32 / N, ROWS = 64 / LANES;      // columns of a lane; lanes of a row; rows of a request
+    const int i = lane % 32, h = lane / 32;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(own + i * 32 + ((4 * h + j) ^ (i & 7)) * 4) = f32x4{sums[4 * j], sums[4 * j + 1], sums[4 * j + 2], sums[4 * j + 3]};
+    const int c = lane % LANES * N;
+#pragma unroll
+    for (int k = 0; k < 32 / ROWS; ++k) {
+        const int row = k * ROWS + lane / LANES;
+        float v[N];
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            const f32x4 p = *reinterpret_cast<const f32x4*>(own + row * 32 + (((c + j) / 4) ^ (row & 7)) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[j + e] = p[e];
+        }
+        store_row<N, BF16>(a, t0 + row, s0 + c, v);
+    }
+}
+
 // NS x NT waves, each RS x RT tiles of 32 x 32; STAGES blocks in LDS, all but one of them on their way.  BF16: the result's
 // type, and with it the instruction.  TILES: W has a scale for 128 x 128.
 //
@@ -262,6 +287,16 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         });                                                                                                       \
         if (step + 1 >= steps) break;                                                                             \
     }
+    if constexpr (STAGES == 1) {
+        static_assert(KG == 1, "one group");
+        for (int b = 0; b < a.kb; ++b) {
+            if (b) meet();
+            fetch(b, st0);
+            wait_loads<0>();
+            meet();
+            compute(st0, [](int) {});
+        }
+    } else {
     const int steps = (a.kb + KG - 1) / KG;
     fetch(min(kg, a.kb - 1), st0);
     if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), st1);
@@ -277,8 +312,10 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
             CRISP_STEP(0, 0, 3) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1) CRISP_STEP(3, 3, 2)
         }
     }
+    }
 #undef CRISP_STEP
     wait_loads<0>();
+    meet();
     if constexpr (KG > 1) {
         static_assert(STAGE >= BS * BT * 4, "a group's sums fit a stage");
         f32x16* part = reinterpret_cast<f32x16*>(st0);
@@ -310,21 +347,19 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         if (kg > 0) return;
     }
 
+    // (a group's sums lay in the stage too: every wave goes on in the place of its own)
+    float* own = reinterpret_cast<float*>(st0 + wave * (KG > 1 ? RS * RT : 1) * 4096);
+    static_assert(KG > 1 || STAGE >= NW * 4096, "a tile a wave");
 #pragma unroll
     for (int r = 0; r < RS; ++r)
 #pragma unroll
-        for (int q = 0; q < RT; ++q) {
-            float v[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) v[j] = acc[r][q][j];
-            store_row<16, BF16>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, v);
-        }
+        for (int q = 0; q < RT; ++q) store_tile<BF16>(a, t0 + (wt * RT + q) * 32, s0 + (ws * RS + r) * 32, acc[r][q], own, lane);
 }
 
 template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
 __global__ __launch_bounds__(64 * NS * NT * KG, 2) void fp8_tiled_kernel(ProductArgs a, int tiles_s, int tiles_t) {
     constexpr int STAGE = Tiles<NS, NT, RS, RT, KG>::STAGE;
-    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16], st3[STAGES > 3 ? STAGE : 16];
+    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGES > 1 ? STAGE : 16], st2[STAGES > 2 ? STAGE : 16], st3[STAGES > 3 ? STAGE : 16];
     tiled_product<NS, NT, RS, RT, STAGES, KG, BF16, TILES>(a, tiles_s, tiles_t, (int)blockIdx.x, st0, st1, st2, st3);
 }
 
