@@ -92,6 +92,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
     constexpr int LW = BS / 8 / NW, LX = BT / 8 / NW;            // requests of eight rows that a wave makes per step
     static_assert(BS % (8 * NW) == 0 && BT % (8 * NW) == 0 && BS % 64 == 0, "whole requests");
     constexpr int PER = LW + LX + LS;
+    constexpr bool DIRECT = BF16 && RS * RT >= 6;                // results leave without changing lanes
     const int lane = threadIdx.x % 64, all = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wave = all % NW, kg = all / NW;                    // (kg is 0 where there is one group)
 
@@ -287,7 +288,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         });                                                                                                       \
         if (step + 1 >= steps) break;                                                                             \
     }
-    if constexpr (STAGES == 1) {
+    if constexpr (STAGES == 1) {                     // other workgroups of the CU work while this one waits
         static_assert(KG == 1, "one group");
         for (int b = 0; b < a.kb; ++b) {
             if (b) meet();
@@ -297,25 +298,25 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
             compute(st0, [](int) {});
         }
     } else {
-    const int steps = (a.kb + KG - 1) / KG;
-    fetch(min(kg, a.kb - 1), st0);
-    if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), st1);
-    if constexpr (AHEAD > 2) fetch(min(2 * KG + kg, a.kb - 1), st2);
-    // (with requests under way at the loop's head the compiler would wait for all of them in each of its rounds)
-    wait_loads<0>();
-    for (int step0 = 0;; step0 += STAGES) {
-        if constexpr (STAGES == 2) {
-            CRISP_STEP(0, 0, 1) CRISP_STEP(1, 1, 0)
-        } else if constexpr (STAGES == 3) {
-            CRISP_STEP(0, 0, 2) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1)
-        } else {
-            CRISP_STEP(0, 0, 3) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1) CRISP_STEP(3, 3, 2)
+        const int steps = (a.kb + KG - 1) / KG;
+        fetch(min(kg, a.kb - 1), st0);
+        if constexpr (AHEAD > 1) fetch(min(KG + kg, a.kb - 1), st1);
+        if constexpr (AHEAD > 2) fetch(min(2 * KG + kg, a.kb - 1), st2);
+        // (with requests under way at the loop's head the compiler would wait for all of them in each of its rounds)
+        wait_loads<0>();
+        for (int step0 = 0;; step0 += STAGES) {
+            if constexpr (STAGES == 2) {
+                CRISP_STEP(0, 0, 1) CRISP_STEP(1, 1, 0)
+            } else if constexpr (STAGES == 3) {
+                CRISP_STEP(0, 0, 2) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1)
+            } else {
+                CRISP_STEP(0, 0, 3) CRISP_STEP(1, 1, 0) CRISP_STEP(2, 2, 1) CRISP_STEP(3, 3, 2)
+            }
         }
-    }
     }
 #undef CRISP_STEP
     wait_loads<0>();
-    meet();
+    if constexpr (!DIRECT) meet();
     if constexpr (KG > 1) {
         static_assert(STAGE >= BS * BT * 4, "a group's sums fit a stage");
         f32x16* part = reinterpret_cast<f32x16*>(st0);
@@ -347,13 +348,23 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         if (kg > 0) return;
     }
 
+    // With six tiles and more a wave the way round by LDS costs 1 to 3 % (4096 x 11008 x 4096, a scale for each W row: 212.5 us against 206).
     // (a group's sums lay in the stage too: every wave goes on in the place of its own)
     float* own = reinterpret_cast<float*>(st0 + wave * (KG > 1 ? RS * RT : 1) * 4096);
     static_assert(KG > 1 || STAGE >= NW * 4096, "a tile a wave");
 #pragma unroll
     for (int r = 0; r < RS; ++r)
 #pragma unroll
-        for (int q = 0; q < RT; ++q) store_tile<BF16>(a, t0 + (wt * RT + q) * 32, s0 + (ws * RS + r) * 32, acc[r][q], own, lane);
+        for (int q = 0; q < RT; ++q) {
+            if constexpr (DIRECT) {
+                float v[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = acc[r][q][j];
+                store_row<16, true>(a, t0 + (wt * RT + q) * 32 + i, s0 + (ws * RS + r) * 32 + 16 * h, v);
+            } else {
+                store_tile<BF16>(a, t0 + (wt * RT + q) * 32, s0 + (ws * RS + r) * 32, acc[r][q], own, lane);
+            }
+        }
 }
 
 template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool TILES>
@@ -373,46 +384,68 @@ __global__ __launch_bounds__(512, 2) void fp8_pair_kernel(ProductArgs a, Product
     else tiled_product<2, 2, 1, 1, 3, 2, false, false>(b, b_s, b_t, (int)blockIdx.x - first, st0, st1, st2, nullptr);
 }
 
-template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16>
+// ALWAYS: W has a scale for 128 x 128, whatever calls.
+template <int NS, int NT, int RS, int RT, int STAGES, int KG, bool BF16, bool ALWAYS = false>
 static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     const int ts = (a.S + NS * RS * 32 - 1) / (NS * RS * 32), tt = (a.T + NT * RT * 32 - 1) / (NT * RT * 32);
-    auto kernel = a.w_tiles || RS * RT == 8 ? fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, true> : fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, RS * RT == 8>;
+    auto kernel = a.w_tiles || ALWAYS ? fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, true> : fp8_tiled_kernel<NS, NT, RS, RT, STAGES, KG, BF16, ALWAYS>;
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT * KG, 0, st>>>(a, ts, tt);
 }
 
-// The tile: the fewest rounds of 256 workgroups (each takes a CU's LDS), each the time of its blocks and of a first request and a
-// last store that nothing hides, in microseconds as measured with 16 x 16 tiles and K = 1024 and 4096.  Results in fp32 have
-// twice the matrix work and the widening, and registers for no more than 128 x 256; W with a scale for each row costs some too
-// (256 x 256 spills).  On 32 sizes of 64 x 256 x 128 to 8192 x 5120 x 256 the rule's choice takes 1 % longer than the best of all, in
-// the geometric mean, 11 % at the most.
+// The tile and its stages by estimated time.  Kernels of one workgroup a CU (their stages fill its LDS) take, for each round of 256 of
+// them, a first request and a last store that nothing hides and a time for each block.  Of those with one or two small stages
+// several run on a CU and hide these from each other: the work of a CU's tiles counts once a tile, or the way through the blocks
+// once for as many as run together.  So small tiles win where the results' way out bounds the time (few blocks) or their number
+// does not fill the last round, large ones where the matrix cores do.
 //
-//   us, K = 4096, 256 tiles:   bf16, W tiles   bf16, W rows   fp32
-//   64 x 64, two groups           11.7            11.8        18.1
-//   128 x 64, two groups          15.9            18.0        27.9
-//   128 x 128                     24.3            28.6        48.6
-//   192 x 128                     31.6            37.4        63.9
-//   128 x 256                     38.9            43.7        85.2
-//   192 x 256                     51.5            58.4
-//   256 x 256                     64.6
-enum { SHAPES = 7 };
+// Constants in microseconds, fitted to the times of 266 sizes of 33 x 33 x 16 to 9000 x 12000 x 9000 for each type; the rule's choices take
+// 2 % longer than the best of twelve to fourteen shapes, in the geometric mean.  A few sizes, us (the rule's choices marked; --: no registers
+// for it; not built: 128 x 64 for bf16, 192 x 128 for fp32, 128 x 256):
+//
+//                          5632 x 2614 x 16   8192 x 5120 x 256    1280 x 3456 x 1840     4096 x 4096 x 4096
+//                           fp32    bf16        fp32    bf16         fp32    bf16           fp32    bf16
+//   64 x 64, two groups     51.3    41.4       135.6   112.4         47.1    32.0          236.3   158.2
+//   64 x 64, one stage      17.3*   11.6*       48.1*   28.8*        30.1    21.2          169.1   109.8
+//   64 x 64, two stages     18.6    14.2        50.4    36.6         31.5*   24.1          169.5   111.1
+//   128 x 64, two stages    19.0    14.1        51.5    36.5         30.7    20.8          157.8    91.9
+//   128 x 128, two stages   21.0    14.5        51.4    36.5         34.9    18.1          142.1*   73.9
+//   the same, 8 waves       23.0    12.8        56.1    29.2         42.7    19.7          167.9    75.2
+//   192 x 128               24.5    17.4        59.1    41.4         31.0    17.3*         163.6    87.8
+//   128 x 256, 3 stages     22.8    15.2        53.3    36.4         36.2    19.9          138.6    75.6
+//   256 x 256                 --    15.9          --    37.6           --    27.4             --    63.3*
+struct Times { float base, tile, block, way; };          // a launch; a tile's ends; a tile's block; a block's way
+struct Shape { int bs, bt, together; Times t[3]; };      // fp32; bf16: W tiles, W rows; 0: not built
+constexpr int SHAPES = 10;
+static const Shape shapes[SHAPES] = {
+    {64, 64, 1, {{1.75f, 2.88f, 0.37f, 0}, {1.76f, 2.45f, 0.215f, 0}, {1.6f, 2.3f, 0.23f, 0}}},               // two groups
+    {64, 64, 5, {{3.33f, 0.56f, 0.32f, 0.74f}, {3.4f, 0.24f, 0.20f, 0.49f}, {3.0f, 0.25f, 0.22f, 0.65f}}},    // one stage
+    {64, 64, 4, {{3.54f, 0.66f, 0.31f, 0.49f}, {2.9f, 0.54f, 0.19f, 0.37f}, {2.93f, 0.47f, 0.205f, 0.38f}}},  // two stages
+    {128, 64, 1, {{}, {1.62f, 3.67f, 0.31f, 0}, {1.44f, 3.78f, 0.35f, 0}}},                                   // two groups
+    {128, 64, 3, {{3.52f, 1.43f, 0.54f, 0.73f}, {}, {}}},                                                     // two stages
+    {128, 128, 1, {{}, {1.21f, 3.90f, 0.48f, 0}, {}}},                                                        // four stages
+    {128, 128, 2, {{3.56f, 3.09f, 0.92f, 1.09f}, {3.12f, 1.77f, 0.49f, 0.52f}, {2.8f, 1.76f, 0.57f, 0.64f}}}, // two stages; bf16: 8 waves
+    {192, 128, 1, {{}, {0.39f, 5.09f, 0.72f, 0}, {0.32f, 5.9f, 0.86f, 0}}},
+    {192, 256, 1, {{}, {0.0f, 8.2f, 1.04f, 0}, {0.0f, 8.3f, 1.3f, 0}}},
+    {256, 256, 1, {{}, {0.0f, 12.0f, 1.25f, 0}, {}}}};
+
+static int type_of(const ProductArgs& a) { return !a.y_bf16 ? 0 : a.w_tiles ? 1 : 2; }
+static int64_t tiles_of(const Shape& s, const ProductArgs& a) { return (int64_t)((a.S + s.bs - 1) / s.bs) * ((a.T + s.bt - 1) / s.bt); }
+
+static float estimate(const Shape& s, const ProductArgs& a) {
+    const Times& t = s.t[type_of(a)];
+    const int64_t m = (tiles_of(s, a) + 255) / 256;
+    const float work = (float)m * t.block, way = (float)((m + s.together - 1) / s.together) * t.way;
+    return t.base + (float)m * t.tile + (float)a.kb * (work > way ? work : way);
+}
+
 static int tile_shape(const ProductArgs& a) {
-    static const struct { int bs, bt; float step[3], rest[3]; } shapes[SHAPES] = {         // fp32; bf16: W tiles, W rows; 0: none
-        {64, 64, {0.42f, 0.22f, 0.23f}, {4.6f, 4.6f, 4.5f}},     {128, 64, {0.65f, 0.34f, 0.41f}, {7.0f, 5.0f, 4.8f}},
-        {128, 128, {1.20f, 0.59f, 0.73f}, {10.3f, 5.4f, 5.4f}},  {192, 128, {1.59f, 0.78f, 0.96f}, {13.0f, 6.5f, 6.7f}},
-        {128, 256, {2.19f, 0.96f, 1.12f}, {15.2f, 8.1f, 8.0f}},  {192, 256, {0.0f, 1.33f, 1.54f}, {0.0f, 9.1f, 9.1f}},
-        {256, 256, {0.0f, 1.68f, 0.0f}, {0.0f, 10.9f, 0.0f}}};
-    const int type = !a.y_bf16 ? 0 : a.w_tiles ? 1 : 2;
     int best = 0;
-    float least = 0.0f;
-    for (int k = 0; k < SHAPES; ++k) {
-        if (shapes[k].step[type] == 0.0f) continue;
-        const int64_t n = (int64_t)((a.S + shapes[k].bs - 1) / shapes[k].bs) * ((a.T + shapes[k].bt - 1) / shapes[k].bt);
-        const float cost = (float)((n + 255) / 256) * ((float)a.kb * shapes[k].step[type] + shapes[k].rest[type]);
-        if (k == 0 || cost < least) { best = k; least = cost; }
-    }
+    for (int k = 1; k < SHAPES; ++k)
+        if (shapes[k].t[type_of(a)].block > 0.0f && estimate(shapes[k], a) < estimate(shapes[best], a)) best = k;
     return best;
 }
 
+// Only where each would run in this shape by itself: two groups add their sums in an order of their own.
 bool fp8_pairs(const ProductArgs& a, const ProductArgs& b) {
     return a.y_bf16 && a.w_tiles && !b.y_bf16 && !b.w_tiles && tile_shape(a) == 0 && tile_shape(b) == 0;
 }
@@ -424,20 +457,21 @@ hipError_t launch_fp8_pair(const ProductArgs& a, const ProductArgs& b, hipStream
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
-    const int best = tile_shape(a);
-    switch (best * 2 + a.y_bf16) {
+    switch (tile_shape(a) * 2 + a.y_bf16) {
         case 0: launch_tiles<2, 2, 1, 1, 3, 2, false>(a, st); break;
         case 1: launch_tiles<2, 2, 1, 1, 3, 2, true>(a, st); break;
-        case 2: launch_tiles<2, 2, 2, 1, 3, 2, false>(a, st); break;
-        case 3: launch_tiles<2, 2, 2, 1, 3, 2, true>(a, st); break;
-        case 4: launch_tiles<2, 4, 2, 1, 4, 1, false>(a, st); break;
-        case 5: launch_tiles<2, 4, 2, 1, 4, 1, true>(a, st); break;
-        case 6: launch_tiles<2, 4, 3, 1, 3, 1, false>(a, st); break;
-        case 7: launch_tiles<2, 4, 3, 1, 3, 1, true>(a, st); break;
-        case 8: launch_tiles<2, 4, 2, 2, 3, 1, false>(a, st); break;
-        case 9: launch_tiles<2, 4, 2, 2, 3, 1, true>(a, st); break;
-        case 11: launch_tiles<2, 4, 3, 2, 2, 1, true>(a, st); break;
-        default: launch_tiles<2, 4, 4, 2, 2, 1, true>(a, st); break;
+        case 2: launch_tiles<2, 2, 1, 1, 1, 1, false>(a, st); break;
+        case 3: launch_tiles<2, 2, 1, 1, 1, 1, true>(a, st); break;
+        case 4: launch_tiles<2, 2, 1, 1, 2, 1, false>(a, st); break;
+        case 5: launch_tiles<2, 2, 1, 1, 2, 1, true>(a, st); break;
+        case 7: launch_tiles<2, 2, 2, 1, 3, 2, true>(a, st); break;
+        case 8: launch_tiles<2, 2, 2, 1, 2, 1, false>(a, st); break;
+        case 11: launch_tiles<2, 4, 2, 1, 4, 1, true, true>(a, st); break;
+        case 12: launch_tiles<2, 2, 2, 2, 2, 1, false>(a, st); break;
+        case 13: launch_tiles<2, 4, 2, 1, 2, 1, true>(a, st); break;
+        case 15: launch_tiles<2, 4, 3, 1, 3, 1, true>(a, st); break;
+        case 17: launch_tiles<2, 4, 3, 2, 2, 1, true>(a, st); break;
+        default: launch_tiles<2, 4, 4, 2, 2, 1, true, true>(a, st); break;
     }
     return hipGetLastError();
 }
