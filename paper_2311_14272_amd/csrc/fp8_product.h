@@ -110,9 +110,9 @@ __device__ __forceinline__ void store_row(const ProductArgs& a, int64_t t, int s
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st);
-// Two products in one launch: whether these are such, and the launch.  Results are those of two launches.
-bool fp8_pairs(const ProductArgs& a, const ProductArgs& b);
-hipError_t launch_fp8_pair(const ProductArgs& a, const ProductArgs& b, hipStream_t st);
+// Two products in one launch: whether (not 0) and how, and the launch.  Results are those of two launches.
+int fp8_pairs(const ProductArgs& a, const ProductArgs& b);
+hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b, hipStream_t st);
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st);
 
 }  // namespace crisp

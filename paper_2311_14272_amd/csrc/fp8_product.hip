@@ -34,7 +34,8 @@ hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, vo
 hipError_t launch_fp8_gradients(const crisp_fp8_mat& G, const crisp_fp8_mat& Wt, void* dX, int64_t lddx, int dx_type, const crisp_fp8_mat& Gt,
                                 const crisp_fp8_mat& Xt, void* dW, int64_t lddw, int dw_type, const crisp_epilogue* ep, hipStream_t st) {
     const ProductArgs a = args_of(G, Wt, dX, lddx, dx_type, nullptr), b = args_of(Gt, Xt, dW, lddw, dw_type, ep);
-    if (!takes_split(a) && !takes_split(b) && fp8_pairs(a, b)) return launch_fp8_pair(a, b, st);
+    const int pairs = takes_split(a) || takes_split(b) ? 0 : fp8_pairs(a, b);
+    if (pairs) return launch_fp8_pair(pairs, a, b, st);
     const hipError_t e = launch_product(a, st);
     return e == hipSuccess ? launch_product(b, st) : e;
 }

@@ -375,13 +375,14 @@ __global__ __launch_bounds__(64 * NS * NT * KG, 2) void fp8_tiled_kernel(Product
 }
 
 // A layer's two gradients in one launch, the input's (bf16, W with a scale for 128 x 128) in the first workgroups, the weight's
-// (fp32, both operands with a scale for each row) in the others: for sizes whose 64 x 64 tiles leave CUs idle.
-__global__ __launch_bounds__(512, 2) void fp8_pair_kernel(ProductArgs a, ProductArgs b, int a_s, int a_t, int b_s, int b_t) {
-    constexpr int STAGE = Tiles<2, 2, 1, 1, 2>::STAGE;
-    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGE];
+// (fp32, both operands with a scale for each row) in the others.
+template <int STAGES, int KG>
+__global__ __launch_bounds__(256 * KG, 2) void fp8_pair_kernel(ProductArgs a, ProductArgs b, int a_s, int a_t, int b_s, int b_t) {
+    constexpr int STAGE = Tiles<2, 2, 1, 1, KG>::STAGE;
+    __shared__ __align__(16) uint8_t st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16];
     const int first = a_s * a_t;
-    if ((int)blockIdx.x < first) tiled_product<2, 2, 1, 1, 3, 2, true, true>(a, a_s, a_t, (int)blockIdx.x, st0, st1, st2, nullptr);
-    else tiled_product<2, 2, 1, 1, 3, 2, false, false>(b, b_s, b_t, (int)blockIdx.x - first, st0, st1, st2, nullptr);
+    if ((int)blockIdx.x < first) tiled_product<2, 2, 1, 1, STAGES, KG, true, true>(a, a_s, a_t, (int)blockIdx.x, st0, st1, st2, nullptr);
+    else tiled_product<2, 2, 1, 1, STAGES, KG, false, false>(b, b_s, b_t, (int)blockIdx.x - first, st0, st1, st2, nullptr);
 }
 
 // ALWAYS: W has a scale for 128 x 128, whatever calls.
@@ -431,28 +432,45 @@ static const Shape shapes[SHAPES] = {
 static int type_of(const ProductArgs& a) { return !a.y_bf16 ? 0 : a.w_tiles ? 1 : 2; }
 static int64_t tiles_of(const Shape& s, const ProductArgs& a) { return (int64_t)((a.S + s.bs - 1) / s.bs) * ((a.T + s.bt - 1) / s.bt); }
 
-static float estimate(const Shape& s, const ProductArgs& a) {
-    const Times& t = s.t[type_of(a)];
-    const int64_t m = (tiles_of(s, a) + 255) / 256;
+static float estimate(const Shape& s, const Times& t, int64_t tiles, int kb) {
+    const int64_t m = (tiles + 255) / 256;
     const float work = (float)m * t.block, way = (float)((m + s.together - 1) / s.together) * t.way;
-    return t.base + (float)m * t.tile + (float)a.kb * (work > way ? work : way);
+    return t.base + (float)m * t.tile + (float)kb * (work > way ? work : way);
 }
 
+static float estimate(int shape, const ProductArgs& a) { return estimate(shapes[shape], shapes[shape].t[type_of(a)], tiles_of(shapes[shape], a), a.kb); }
+
+// Two groups add their sums in an order of their own; the other shapes have the same bits.
+static bool grouped(int shape) { return shape == 0 || shape == 3; }
+
+// Two groups from twelve blocks on: at nine they gain 0.2 to 0.5 us (512 x 512 x 1152: 6.1 against 6.3, fp32 7.5 against 8.0), and a layer's two
+// gradients, one of them of few blocks, then rarely have a launch in common (256 x 1024 x 1024 with the quantiser: 14.9 us apart, 12.3 together).
 static int tile_shape(const ProductArgs& a) {
-    int best = 0;
-    for (int k = 1; k < SHAPES; ++k)
-        if (shapes[k].t[type_of(a)].block > 0.0f && estimate(shapes[k], a) < estimate(shapes[best], a)) best = k;
+    int best = -1;
+    for (int k = 0; k < SHAPES; ++k) {
+        if (shapes[k].t[type_of(a)].block == 0.0f || (grouped(k) && a.kb < 12)) continue;
+        if (best < 0 || estimate(k, a) < estimate(best, a)) best = k;
+    }
     return best;
 }
 
-// Only where each would run in this shape by itself: two groups add their sums in an order of their own.
-bool fp8_pairs(const ProductArgs& a, const ProductArgs& b) {
-    return a.y_bf16 && a.w_tiles && !b.y_bf16 && !b.w_tiles && tile_shape(a) == 0 && tile_shape(b) == 0;
+// Two products in one launch of 64 x 64 tiles, of two groups or of two stages: where neither result changes by it and that takes less time
+// than two launches.  0: not.
+int fp8_pairs(const ProductArgs& a, const ProductArgs& b) {
+    if (!a.y_bf16 || !a.w_tiles || b.y_bf16 || b.w_tiles) return 0;
+    const int sa = tile_shape(a), sb = tile_shape(b);
+    if (grouped(sa) != grouped(sb)) return 0;
+    const int k = grouped(sa) ? 0 : 2;
+    const int64_t tiles = tiles_of(shapes[k], a) + tiles_of(shapes[k], b);
+    const float ea = estimate(shapes[k], shapes[k].t[1], tiles, a.kb), eb = estimate(shapes[k], shapes[k].t[0], tiles, b.kb);
+    return (ea > eb ? ea : eb) < estimate(sa, a) + estimate(sb, b) ? 2 - grouped(sa) : 0;
 }
 
-hipError_t launch_fp8_pair(const ProductArgs& a, const ProductArgs& b, hipStream_t st) {
+hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b, hipStream_t st) {
     const int as = (a.S + 63) / 64, at = (a.T + 63) / 64, bs = (b.S + 63) / 64, bt = (b.T + 63) / 64;
-    fp8_pair_kernel<<<(unsigned)(as * at + bs * bt), 512, 0, st>>>(a, b, as, at, bs, bt);
+    const unsigned grid = (unsigned)(as * at + bs * bt);
+    if (pairs == 1) fp8_pair_kernel<3, 2><<<grid, 512, 0, st>>>(a, b, as, at, bs, bt);
+    else fp8_pair_kernel<2, 1><<<grid, 256, 0, st>>>(a, b, as, at, bs, bt);
     return hipGetLastError();
 }
 

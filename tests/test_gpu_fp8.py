@@ -328,7 +328,7 @@ def test_long_offsets():
 
 # ---- the layer's gradients ----------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("shape", [(1, 130, 260), (40, 128, 256), (200, 300, 140), (513, 256, 129), (260, 640, 384)], ids=str)
+@pytest.mark.parametrize("shape", [(1, 130, 260), (40, 128, 256), (200, 300, 140), (513, 256, 129), (260, 640, 384), (1700, 1500, 140), (500, 512, 1152), (1700, 300, 300)], ids=str)
 def test_backward(shape):
     T, S, K = shape
     print("backward", shape, flush=True)
