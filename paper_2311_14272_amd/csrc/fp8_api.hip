@@ -32,7 +32,7 @@ static crisp_status check_out(const void* Y, int64_t T, int64_t S, int64_t most_
     if (off(Y, size)) return CRISP_EALIGN;
     // a launch takes fewer than 2^32 threads: up to 1024 for 16 x 16 results, or 512 for 64 x 64
     const int64_t tiles = ((T + 15) / 16) * ((S + 15) / 16);
-    if (tiles > (fp8_takes_split(T, S, most_ld) ? ((int64_t)1 << 22) - 1 : ((int64_t)1 << 26))) return CRISP_ESHAPE;
+    if (tiles > (fp8_may_split(T, S, most_ld) ? ((int64_t)1 << 22) - 1 : ((int64_t)1 << 26))) return CRISP_ESHAPE;
     if (!ep) return CRISP_OK;
     if (ep->relu != 0 && ep->relu != 1) return CRISP_EINVAL;
     if (ep->residual && (ep->ldr < S || ep->ldr > MOST_LD)) return CRISP_ESHAPE;

@@ -8,8 +8,8 @@ namespace crisp {
 
 hipError_t launch_fp8_quant(const void* X, int in_type, int64_t rows, int64_t cols, int64_t ldx, const uint32_t* mask,
                             const crisp_fp8_mat* Q, const crisp_fp8_mat* Qt, hipStream_t st);
-// Whether the product of T x K and S x K runs without staging; ld: the larger row stride.
-inline bool fp8_takes_split(int64_t T, int64_t S, int64_t ld) { return T <= 32 || S <= 32 || ld >= 1 << 24; }
+// Whether the product of T x K and S x K may run without staging; ld: the larger row stride.
+inline bool fp8_may_split(int64_t T, int64_t S, int64_t ld) { return T <= 32 || S <= 32 || ld >= 1 << 24; }
 hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
                               const crisp_epilogue* ep, hipStream_t st);
 

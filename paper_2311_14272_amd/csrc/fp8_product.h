@@ -114,5 +114,8 @@ hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st);
 int fp8_pairs(const ProductArgs& a, const ProductArgs& b);
 hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b, hipStream_t st);
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st);
+// Microseconds that either kernel is expected to take.
+float fp8_tiled_time(const ProductArgs& a);
+float fp8_split_time(const ProductArgs& a);
 
 }  // namespace crisp

@@ -19,11 +19,18 @@ static ProductArgs args_of(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void*
     return a;
 }
 
-static bool takes_split(const ProductArgs& a) { return fp8_takes_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw); }
+// Few rows of X or of W: no staging, the waves split the contraction - but where many rows of the other one fill the CUs with tiles (32 x 28672 x
+// 4096, us: 28 against 45; 32 x 4096 x 11008: 27 against 22; 16384 x 32 x 4096: 14 against 20).  The tiled kernel's estimate is for
+// operands in the caches; from memory bf16 results take 1.1 times as long (fp32, bound by the widening, 0.95), and no less than the reads at
+// 4.3 TB/s.  What one launch could have done
+// together with the quantiser is summed in that launch's order.  The tiled kernels' offsets inside a tile are 32 bits.
+static bool takes_split(const ProductArgs& a) {
+    if (!fp8_may_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw)) return false;
+    if (a.ldx >= 1 << 24 || a.ldw >= 1 << 24 || fp8_takes_raw(a.T, a.K)) return true;
+    const float tiled = (a.y_bf16 ? 1.1f : 0.95f) * fp8_tiled_time(a), read = 2.0f + ((float)a.T + (float)a.S) * (float)a.kb * (128e-6f / 4.3f);
+    return fp8_split_time(a) < (tiled > read ? tiled : read);
+}
 
-// Up to 32 rows of X are read by every workgroup and the weights bound the time: no staging (S = K = 4096, us, from memory: 16
-// rows 6.5 against 12 with 64 x 64 tiles, 32: 9.2 and 11.7, 64: 12.6 and 13.0, 128: 18.9 and 12.7; from the caches 64: 10.7 and
-// 9.4).  So is a W of few rows: X is then what is read.  The tiled kernels' offsets inside a tile are 32 bits.
 static hipError_t launch_product(const ProductArgs& a, hipStream_t st) { return takes_split(a) ? launch_fp8_split(a, st) : launch_fp8_tiled(a, st); }
 
 hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,

@@ -454,6 +454,8 @@ static int tile_shape(const ProductArgs& a) {
     return best;
 }
 
+float fp8_tiled_time(const ProductArgs& a) { return estimate(tile_shape(a), a); }
+
 // Two products in one launch of 64 x 64 tiles, of two groups or of two stages: where neither result changes by it and that takes less time
 // than two launches.  0: not.
 int fp8_pairs(const ProductArgs& a, const ProductArgs& b) {

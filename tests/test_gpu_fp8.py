@@ -168,7 +168,8 @@ PRODUCTS = [(1, 1, 1), (1, 16, 128), (2, 48, 100), (1, 1000, 4096), (5, 130, 640
             (256, 256, 256), (333, 1000, 130), (512, 512, 1152), (700, 384, 2304), (1030, 1025, 140),
             (3400, 3841, 260), (4096, 4096, 128), (20, 60, 9000), (1000, 40, 300), (90, 70, 200), (1100, 2000, 384),
             (2100, 2050, 200), (65, 65, 65), (80, 96, 1000), (1280, 3456, 130), (1270, 3400, 390), (2300, 4900, 130), (67, 8475, 2879), (265, 9836, 554),
-            (195, 8281, 1074), (4947, 1409, 258), (5530, 919, 386), (4267, 2690, 130), (1864, 7758, 261)]
+            (195, 8281, 1074), (4947, 1409, 258), (5530, 919, 386), (4267, 2690, 130), (1864, 7758, 261),
+            (24, 9000, 300), (9000, 24, 300), (20, 3000, 4200), (3000, 20, 4200), (30, 700, 1000), (16, 12000, 1100)]
 
 
 @pytest.mark.parametrize("w_tiles", [True, False], ids=["tiles", "rows"])
