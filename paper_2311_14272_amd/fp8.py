@@ -36,6 +36,7 @@ _pack = struct.Struct("@PPqqqqii").pack          # a crisp_fp8_mat as bytes: a t
 _pack_ep = struct.Struct("@PPPqii").pack         # and a crisp_epilogue
 
 _lib = None
+_device = torch._C._cuda_getDevice
 
 
 def lib():
@@ -68,13 +69,13 @@ def _backward_ws(T, S):
 
 def _here(t, what):
     """A tensor's address; it has to be on the device whose stream the work goes to."""
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != _device():              # (-1 for a tensor of the host)
         raise ValueError("%s is on %s, not on the current GPU" % (what, t.device))
     return t.data_ptr()
 
 
 def _mats_here(*mats):
-    now = torch._C._cuda_getDevice()
+    now = _device()
     for m in mats:
         if m is not None and m.dev != now:
             raise ValueError("a matrix is on GPU %d, not on the current one" % m.dev)
@@ -172,12 +173,14 @@ def quantize_both(x, kind=ROWS, mask=None, out=None, out_t=None):
     return out, out_t
 
 
-def _output(T, S, out, out_dtype, device):
+def _output(T, S, out, out_dtype, device, what="out"):
+    """(the result's tensor, its address, its row stride)"""
     if out is None:
-        return torch.empty_strided((T, S), (S, 1), dtype=out_dtype, device=device)
+        out = torch.empty_strided((T, S), (S, 1), dtype=out_dtype, device=device)
+        return out, out.data_ptr(), S
     if out.dtype not in _IN or tuple(out.shape) != (T, S) or (S > 1 and out.stride(1) != 1):
-        raise ValueError("out: %d x %d of fp32 or bf16 with contiguous rows" % (T, S))
-    return out
+        raise ValueError("%s: %d x %d of fp32 or bf16 with contiguous rows" % (what, T, S))
+    return out, _here(out, what), out.stride(0) if T > 1 else max(out.stride(0), S)
 
 
 def _epilogue(ep, bias, S):
@@ -191,17 +194,13 @@ def _epilogue(ep, bias, S):
     return _pack_ep(0, _here(bias, "bias"), 0, 0, 0, 0)
 
 
-def _ld(y):
-    return y.stride(0) if y.shape[0] > 1 else max(y.stride(0), y.shape[1])
-
-
 def product(x: Fp8Mat, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None):
     """crisp_fp8_product: x w^T, x.rows x w.rows; into out, allocated as out_dtype when not given.  ep: crisp.epilogue(...),
     per column of the result."""
     _mats_here(x, w)
-    out = _output(x.rows, w.rows, out, out_dtype, x.q.device)
+    out, to, ldy = _output(x.rows, w.rows, out, out_dtype, x.q.device)
     ep = _epilogue(ep, bias, w.rows)
-    st = (_lib or lib()).crisp_fp8_product(x.c, w.c, _here(out, "out"), _ld(out), _IN[out.dtype], ep, crisp._stream())
+    st = (_lib or lib()).crisp_fp8_product(x.c, w.c, to, ldy, _IN[out.dtype], ep, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_product", st)
     return out
@@ -214,14 +213,18 @@ def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None,
     if K != w.cols:
         raise ValueError("x has %d columns, the weights %d" % (K, w.cols))
     _mats_here(w)
-    out = _output(T, w.rows, out, out_dtype, x.device)
-    ep = _epilogue(ep, bias, w.rows)
+    out, to, ldy = _output(T, w.rows, out, out_dtype, x.device)
+    if ep is not None or bias is not None:
+        ep = _epilogue(ep, bias, w.rows)
     if ws is None:
-        need = _linear_ws(T, K)
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
-    st = (_lib or lib()).crisp_fp8_linear(p, kind, T, ldx, w.c, _here(out, "out"), _ld(out), _IN[out.dtype], ep,
-                                          None if ws is None else _here(ws, "ws"), 0 if ws is None else ws.numel() * ws.element_size(),
-                                          crisp._stream())
+        room = _linear_ws(T, K)
+        at = None
+        if room:
+            ws = torch.empty_strided((room,), (1,), dtype=torch.uint8, device=x.device)
+            at = ws.data_ptr()
+    else:
+        at, room = _here(ws, "ws"), ws.numel() * ws.element_size()
+    st = (_lib or lib()).crisp_fp8_linear(p, kind, T, ldx, w.c, to, ldy, _IN[out.dtype], ep, at, room, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_linear", st)
     return out
@@ -239,17 +242,22 @@ def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=F
         raise ValueError("accumulate adds to a dw that is given; dx needs w_t, dw needs x_t")
     _mats_here(x_t, w_t)
     L = _lib or lib()
+    to_x = to_w = None
+    ldx = ldw = tx = tw = 0
     if w_t is not None:
-        dx = _output(T, w_t.rows, dx, torch.bfloat16, dy.device)
+        dx, to_x, ldx = _output(T, w_t.rows, dx, torch.bfloat16, dy.device, "dx")
+        tx = _IN[dx.dtype]
     if x_t is not None:
-        dw = _output(S, x_t.rows, dw, torch.float32, dy.device)
+        dw, to_w, ldw = _output(S, x_t.rows, dw, torch.float32, dy.device, "dw")
+        tw = _IN[dw.dtype]
     if ws is None:
-        ws = torch.empty(max(16, _backward_ws(T, S)), dtype=torch.uint8, device=dy.device)
-    none = (None, 0, 0)
-    st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, x_t and x_t.c, w_t and w_t.c,
-                                     *(none if dx is None else (_here(dx, "dx"), _ld(dx), _IN[dx.dtype])),
-                                     *(none if dw is None else (_here(dw, "dw"), _ld(dw), _IN[dw.dtype])), int(accumulate),
-                                     _here(ws, "ws"), ws.numel() * ws.element_size(), crisp._stream())
+        room = max(16, _backward_ws(T, S))
+        ws = torch.empty_strided((room,), (1,), dtype=torch.uint8, device=dy.device)
+        at = ws.data_ptr()
+    else:
+        at, room = _here(ws, "ws"), ws.numel() * ws.element_size()
+    st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, x_t and x_t.c, w_t and w_t.c, to_x, ldx, tx, to_w, ldw, tw, int(accumulate),
+                                     at, room, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_linear_backward", st)
     return dx, dw
