@@ -98,6 +98,23 @@ def test_masked(shape, types):
     assert torch.equal(c.w[gone], before[gone])
 
 
+def test_masked_rows_of_any_length():
+    """Eight elements that lie in one, two or many rows, and in one or two words of a mask's row; the bits behind a row's end are set
+    and not looked at."""
+    rng = np.random.default_rng(12)
+    cases, tensors = [], []
+    for row in [*range(1, 72), 127, 129, 250, 511]:
+        c = Case(rng, row * int(rng.integers(1, 41)), True, True, 32, row=row)
+        c.g[torch.from_numpy(~c.keep).cuda()] = float("nan")
+        if row % 32:
+            c.mask.view(-1, -(-row // 32))[:, -1] |= -1 << (row % 32)
+        cases.append(c)
+    want = [c.plain(HYPER) for c in cases]
+    adamw.step(adamw.make_batch([c.tensor() for c in cases]), **HYPER)
+    for c, w in zip(cases, want):
+        c.check(w)
+
+
 def test_many_tensors_of_all_types():
     """More tensors than a launch takes, of all types and sizes mixed, empty ones among them; one that comes twice in a
     different place would overlap, so each has its own buffers, cut from one so that what lies between them is seen to stay."""
