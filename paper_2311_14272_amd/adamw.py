@@ -15,7 +15,7 @@ import ctypes as C
 import torch
 
 from . import crisp
-from .fp8 import _here
+from .fp8 import CODES, _here
 
 BLOCK = 128
 _P = {torch.float32: 0, torch.bfloat16: 1}      # CRISP_P_*
@@ -65,9 +65,9 @@ def tensor(w, g, m, v, m_scale=None, v_scale=None, w_copy=None, mask=None, row_l
         raise ValueError("weights and gradients are fp32 or bf16")
     if g.numel() != n or m.numel() != n or v.numel() != n or (w_copy is not None and w_copy.numel() != n):
         raise ValueError("weights, gradients and moments are of one size")
-    if eight and (m_scale is None or v_scale is None or m.element_size() != 1 or v.element_size() != 1
+    if eight and (m_scale is None or v_scale is None or m.dtype not in CODES or v.dtype not in CODES
                   or any(s.dtype != torch.float32 or s.numel() != -(-n // BLOCK) for s in (m_scale, v_scale))):
-        raise ValueError("8-bit moments: one byte an element, and an fp32 scale for each %d elements in m_scale and v_scale" % BLOCK)
+        raise ValueError("8-bit moments: e4m3 codes (float8_e4m3fn or uint8), and an fp32 scale for each %d elements in m_scale and v_scale" % BLOCK)
     if not eight and (m.dtype != torch.float32 or v.dtype != torch.float32):
         raise ValueError("moments without scales are fp32")
     if w_copy is not None and (w_copy.element_size() != 2 or w_copy.dtype not in (torch.bfloat16, torch.int16) or w.dtype != torch.float32):

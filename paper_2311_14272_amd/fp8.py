@@ -24,6 +24,7 @@ from . import crisp
 ROWS, TILES = 0, 1
 BLOCK = 128
 _IN = {torch.float32: 0, torch.bfloat16: 1}     # CRISP_IN_*, and the CRISP_Y_* of the same types
+CODES = (torch.float8_e4m3fn, torch.uint8)      # what holds e4m3 codes: other 8-bit formats have other values for the same byte
 
 
 class _Mat(C.Structure):
@@ -95,8 +96,8 @@ class Fp8Mat:
         if kind not in (ROWS, TILES):
             raise ValueError("kind is ROWS or TILES")
         want = (_blocks(cols), rows) if kind == ROWS else (_blocks(rows), _blocks(cols))
-        if q.dim() != 2 or q.element_size() != 1 or q.shape[0] != rows or q.shape[1] < _blocks(cols) * BLOCK or q.stride(1) != 1:
-            raise ValueError("q: %d rows of at least %d bytes, each row contiguous" % (rows, _blocks(cols) * BLOCK))
+        if q.dtype not in CODES or q.dim() != 2 or q.shape[0] != rows or q.shape[1] < _blocks(cols) * BLOCK or q.stride(1) != 1:
+            raise ValueError("q: %d rows of at least %d e4m3 codes (float8_e4m3fn or uint8), each row contiguous" % (rows, _blocks(cols) * BLOCK))
         if scale.dtype != torch.float32 or scale.dim() != 2 or tuple(scale.shape) != want or (scale.stride(1) != 1 and want[1] > 1):
             raise ValueError("scale: %d x %d fp32, each row contiguous" % want)
         self._fill(q, scale, rows, cols, kind)

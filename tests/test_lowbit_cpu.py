@@ -191,6 +191,27 @@ def test_tensors_off_the_gpu_are_refused():
         adamw.make_batch([])
 
 
+OTHER_BYTES = [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.int8, torch.bool]
+
+
+@pytest.mark.parametrize("other", OTHER_BYTES, ids=str)
+def test_bytes_of_another_type_are_refused(other, monkeypatch):
+    """A byte of another format stands for another value: only uint8 (codes) and float8_e4m3fn are taken."""
+    monkeypatch.setattr(fp8, "_device", lambda: -1)      # tensors of the host count as on the current device
+    scale = torch.zeros((1, 4))
+    m = lambda dtype: torch.zeros(4 * 128, dtype=torch.uint8).view(dtype)
+    x, s = torch.zeros(4 * 128), torch.zeros(4)
+    for good in (torch.uint8, torch.float8_e4m3fn):
+        fp8.Fp8Mat(m(good).view(4, 128), scale, 4, 128, fp8.ROWS)
+        adamw.tensor(x, x, m(good), m(good), m_scale=s, v_scale=s)
+        with pytest.raises(ValueError, match="8-bit moments"):
+            adamw.tensor(x, x, m(good), m(other), m_scale=s, v_scale=s)
+        with pytest.raises(ValueError, match="8-bit moments"):
+            adamw.tensor(x, x, m(other), m(good), m_scale=s, v_scale=s)
+    with pytest.raises(ValueError, match="^q: "):
+        fp8.Fp8Mat(m(other).view(4, 128), scale, 4, 128, fp8.ROWS)
+
+
 def test_plain_e4m3_rounding():
     """All 256 codes stand for themselves; values between two neighbours go to the nearer one, the middle to the even one."""
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
