@@ -75,6 +75,13 @@ def _here(t, what):
     return t.data_ptr()
 
 
+def _workspace(ws):
+    """(address, bytes) of a caller's workspace: bytes one behind the other."""
+    if not ws.is_contiguous():
+        raise ValueError("ws is not contiguous")
+    return _here(ws, "ws"), ws.numel() * ws.element_size()
+
+
 def _mats_here(*mats):
     now = _device()
     for m in mats:
@@ -208,7 +215,7 @@ def product(x: Fp8Mat, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None,
 
 
 def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None, ws=None):
-    """crisp_fp8_linear: the layer for activations x (T x K, fp32 or bf16).  ws: a workspace of the caller's (uint8,
+    """crisp_fp8_linear: the layer for activations x (T x K, fp32 or bf16).  ws: a workspace of the caller's (contiguous,
     crisp_fp8_linear_ws bytes); allocated for the call when not given."""
     p, kind, T, K, ldx = _input(x)
     if K != w.cols:
@@ -224,7 +231,7 @@ def linear(x, w: Fp8Mat, out=None, out_dtype=torch.bfloat16, bias=None, ep=None,
             ws = torch.empty_strided((room,), (1,), dtype=torch.uint8, device=x.device)
             at = ws.data_ptr()
     else:
-        at, room = _here(ws, "ws"), ws.numel() * ws.element_size()
+        at, room = _workspace(ws)
     st = (_lib or lib()).crisp_fp8_linear(p, kind, T, ldx, w.c, to, ldy, _IN[out.dtype], ep, at, room, crisp._stream())
     if st != crisp.OK:
         raise crisp.CrispError("crisp_fp8_linear", st)
@@ -256,7 +263,7 @@ def linear_backward(dy, x_t: Fp8Mat, w_t: Fp8Mat, dx=None, dw=None, accumulate=F
         ws = torch.empty_strided((room,), (1,), dtype=torch.uint8, device=dy.device)
         at = ws.data_ptr()
     else:
-        at, room = _here(ws, "ws"), ws.numel() * ws.element_size()
+        at, room = _workspace(ws)
     st = L.crisp_fp8_linear_backward(p, kind, T, S, ldg, x_t and x_t.c, w_t and w_t.c, to_x, ldx, tx, to_w, ldw, tw, int(accumulate),
                                      at, room, crisp._stream())
     if st != crisp.OK:

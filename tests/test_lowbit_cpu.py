@@ -212,6 +212,34 @@ def test_bytes_of_another_type_are_refused(other, monkeypatch):
         fp8.Fp8Mat(m(other).view(4, 128), scale, 4, 128, fp8.ROWS)
 
 
+def test_workspaces_that_are_not_a_row_of_bytes(monkeypatch):
+    """A strided workspace has room between its elements that is not the caller's to give, an expanded one has none at all."""
+    monkeypatch.setattr(fp8, "_device", lambda: -1)
+    monkeypatch.setattr(crisp, "_stream", lambda: None)
+    reached = []
+
+    class Library:
+        """Takes every call and enqueues nothing."""
+        def __getattr__(self, name):
+            return lambda *args: reached.append(name) or crisp.OK
+
+    room = max(fp8.lib().crisp_fp8_linear_ws(70, 200), fp8.lib().crisp_fp8_linear_backward_ws(70, 64))
+    monkeypatch.setattr(fp8, "_lib", Library())
+    codes = lambda *shape: torch.zeros(shape, dtype=torch.uint8)
+    x, dy = torch.zeros((70, 200)), torch.zeros((70, 64))
+    w = fp8.Fp8Mat(codes(64, 256), torch.zeros((2, 64)), 64, 200, fp8.ROWS)
+    w_t = fp8.Fp8Mat(codes(200, 128), torch.zeros((1, 200)), 200, 64, fp8.ROWS)
+    for good in (codes(room), codes(2, room).view(torch.int16), codes(2, room)[1:]):
+        fp8.linear(x, w, ws=good)
+        fp8.linear_backward(dy, None, w_t, ws=good)
+    assert reached == ["crisp_fp8_linear", "crisp_fp8_linear_backward"] * 3
+    for bad in (codes(1).expand(room), codes(2 * room)[::2], codes(room, 2).t()):
+        with pytest.raises(ValueError, match="ws"):
+            fp8.linear(x, w, ws=bad)
+        with pytest.raises(ValueError, match="ws"):
+            fp8.linear_backward(dy, None, w_t, ws=bad)
+
+
 def test_plain_e4m3_rounding():
     """All 256 codes stand for themselves; values between two neighbours go to the nearer one, the middle to the even one."""
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
