@@ -46,7 +46,7 @@ typedef struct {
 } crisp_adamw_live;
 
 typedef struct {
-    double lr, beta1, beta2, eps;  /* lr >= 0, 0 <= beta < 1, eps > 0                                              */
+    double lr, beta1, beta2, eps;  /* lr >= 0, 0 <= beta < 1, eps > 0 also when rounded to fp32 (more than 2^-150) */
     double grad_scale;             /* gradients are multiplied by this first (clipping, a loss's scale)            */
     int64_t step;                  /* 1 .. 2^31 - 1: number of this step, for the correction of the moments' start */
     const crisp_adamw_live *live;  /* device, 4-byte aligned, or NULL: given, its lr, grad_scale and step replace  */

@@ -294,7 +294,7 @@ extern "C" {
 crisp_status crisp_adamw_batch(int32_t n_tensors, const crisp_adamw_tensor* tensors, const crisp_adamw_hyper* hyper, void* stream) {
     if (n_tensors < 1 || n_tensors > 1 << 20 || !tensors || !hyper) return CRISP_EINVAL;
     const crisp_adamw_hyper& h = *hyper;
-    if (!(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0) || !(h.eps > 0.0 && h.eps <= 1e30)) return CRISP_EINVAL;
+    if (!(h.beta1 >= 0.0 && h.beta1 < 1.0) || !(h.beta2 >= 0.0 && h.beta2 < 1.0) || !((float)h.eps > 0.0f && h.eps <= 1e30)) return CRISP_EINVAL;
     if (!h.live) {
         if (!(h.lr >= 0.0 && h.lr <= 1e30) || !(h.grad_scale >= -1e30 && h.grad_scale <= 1e30)) return CRISP_EINVAL;
         if (h.step < 1 || h.step > INT32_MAX) return CRISP_EINVAL;

@@ -164,6 +164,15 @@ def test_adamw_refusals():
     assert adamw.lib().crisp_adamw_batch(1, None, None, None) == crisp.EINVAL
 
 
+def test_adamw_eps_that_rounds_to_zero():
+    """The step divides by the root plus eps in fp32: an eps that is zero there makes NaN of every element without a gradient."""
+    h = lambda eps: _adamw(h=dict(eps=eps), numel=0)     # (nothing is enqueued for tensors without elements)
+    for bad in (1e-50, 1e-300, 5e-324, 2.0 ** -150):
+        assert h(bad) == crisp.EINVAL, bad
+    for good in (2.0 ** -149, 1e-40, 1e-8, 1e30):
+        assert h(good) == crisp.OK, good
+
+
 def test_hybrid_mask_refusals():
     L = adamw.lib()
     d = crisp.layer_desc(64, 128, 2, 4, 32, 0.5)
