@@ -31,6 +31,17 @@ __device__ __forceinline__ void wait_loads() {
     __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | 0 << 8 | (LEFT >> 4) << 14);
 }
 
+// That wait, and the barrier: behind it no wave of the workgroup still reads what it read before, and the requests that the wait
+// covered have arrived for all of them.  (The compiler moves no access of memory across an empty asm; it emits nothing.)
+template <int LEFT>
+__device__ __forceinline__ void wait_and_meet() {
+    asm volatile("" ::: "memory");
+    wait_loads<LEFT>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // A wave's 32 x 32 results, register j of lane (i, h) row t0 + i and column s0 + 16h + j, through the epilogue and out.  They change
 // lanes in LDS (4 KiB of the wave's own) so that a request writes whole rows of the tile: as 16 bytes here and there they left at
 // 2 TB/s.
@@ -70,12 +81,6 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int t0, int s0,
 // One object of LDS a stage: W's rows, X's rows, scales.  The compiler tells requests to LDS apart by the object that they write,
 // no more than eight of them, and follows few address steps from an object: every address here is an object and one offset.  Where
 // it cannot tell, a read of LDS waits for all requests.
-__device__ __forceinline__ void meet() {
-    asm volatile("" ::: "memory");           // (the compiler moves no access of LDS across; it emits nothing)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 template <int NS, int NT, int RS, int RT, int KG>
 struct Tiles {
     static constexpr int NW = NS * NT, BS = NS * RS * 32, BT = NT * RT * 32;
@@ -279,8 +284,7 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
     {                                                                                                             \
         const int step = step0 + k, b = step * KG + kg;                                                           \
         const int ahead = min(b + AHEAD * KG, a.kb - 1);                                                          \
-        wait_loads<(AHEAD - 1) * PER>();                                                                          \
-        meet();                                                                                                   \
+        wait_and_meet<(AHEAD - 1) * PER>();                                                                       \
         if (KG > 1 && b >= a.kb) break;               /* the last step may have no block for the later groups */  \
         compute(st##here, [&](int tile) {                                                                         \
             _Pragma("unroll") for (int n = 0; n < PER; ++n)                                                       \
@@ -291,10 +295,9 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
     if constexpr (STAGES == 1) {                     // other workgroups of the CU work while this one waits
         static_assert(KG == 1, "one group");
         for (int b = 0; b < a.kb; ++b) {
-            if (b) meet();
+            if (b) wait_and_meet<0>();               // (the block's reads are done in every wave: its place may be written)
             fetch(b, st0);
-            wait_loads<0>();
-            meet();
+            wait_and_meet<0>();
             compute(st0, [](int) {});
         }
     } else {
@@ -315,8 +318,8 @@ __device__ __forceinline__ void tiled_product(const ProductArgs& a, int tiles_s,
         }
     }
 #undef CRISP_STEP
-    wait_loads<0>();
-    if constexpr (!DIRECT) meet();
+    if constexpr (DIRECT) wait_loads<0>();
+    else wait_and_meet<0>();
     if constexpr (KG > 1) {
         static_assert(STAGE >= BS * BT * 4, "a group's sums fit a stage");
         f32x16* part = reinterpret_cast<f32x16*>(st0);

@@ -249,6 +249,19 @@ def test_workspaces_that_are_not_a_row_of_bytes(monkeypatch):
             fp8.linear_backward(dy, None, w_t, ws=bad)
 
 
+def test_barriers_of_the_product_wait_first():
+    """The barrier behind which another wave may overwrite LDS is a bare one: it says nothing about a wave's own reads.  It stands in one
+    function only, after the wait for them."""
+    csrc = os.path.join(ROOT, "paper_2311_14272_amd", "csrc")
+    text = "".join(open(os.path.join(csrc, n)).read() for n in sorted(os.listdir(csrc)) if n.startswith("fp8_"))
+    bodies = re.findall(r"__forceinline__ void \w+\(\) \{(.*?)\n\}", text, re.S)
+    have = [b for b in bodies if "s_barrier" in b]
+    assert len(have) == 1 and text.count("s_barrier") == 1
+    assert re.search(r'asm volatile\(""[^;]*"memory"\);.*wait_loads<LEFT>\(\);.*s_barrier\(\);.*asm volatile\(""[^;]*"memory"\);', have[0], re.S)
+    wait = next(b for b in bodies if "s_waitcnt" in b)
+    assert "LEFT & 15) | 7 << 4 | 0 << 8 |" in wait          # no LDS operation outstanding, however many requests may be
+
+
 def test_plain_e4m3_rounding():
     """All 256 codes stand for themselves; values between two neighbours go to the nearer one, the middle to the even one."""
     codes = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy().astype(np.float64)
