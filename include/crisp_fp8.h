@@ -72,7 +72,8 @@ CRISP_API crisp_status crisp_fp8_quant(const void *X, int32_t in_type, int64_t r
  *   Y: T x ldy, fp32 or bf16 per y_type (CRISP_Y_*), ldy >= S, aligned to its element; every element of the T x S part is
  *      written, none behind it.
  *   ep: the epilogue of crisp_spmm_ep or NULL; scale and bias are per column of Y (S values), residual is T x ldr of Y's
- *      type, ldr >= S, aligned to its element, and may be Y itself (with ldr == ldy): gradients accumulate.
+ *      type, ldr >= S, aligned to its element, and may be Y itself (with ldr == ldy): gradients accumulate.  relu lets NaN
+ *      through.
  * At most 2^26 tiles of 16 x 16 outputs, 2^22 - 1 where T or S is up to 32 or a row stride 2^24 or more (ESHAPE beyond).
  * The sum's order depends on sizes, types and row strides only: the same call gives the same bits.
  * Errors: EINVAL, ESHAPE, EALIGN, EDEVICE.

@@ -83,7 +83,7 @@ __device__ __forceinline__ void store_row(const ProductArgs& a, int64_t t, int s
     }
     if (a.relu) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = fmaxf(v[j], 0.0f);
+        for (int j = 0; j < N; ++j) v[j] = v[j] <= 0.0f ? 0.0f : v[j];      // (fmaxf would make zeros of NaN)
     }
     const int64_t at = t * a.ldy + s;
     if (s + N <= a.S) {

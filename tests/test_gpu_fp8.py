@@ -251,6 +251,24 @@ def test_product_keeps_rows_apart():
     assert y[bad].isnan().all() and torch.equal(y[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 40, 200), (20, 70, 3000), (150, 140, 400), (2300, 4900, 130)], ids=str)
+def test_relu_lets_nan_through(shape, dtype):
+    """A NaN or an infinity in a block makes NaN of the results that use it, behind a ReLU too; the others are as without them."""
+    T, S, K = shape
+    rng = np.random.default_rng(T)
+    x, w = rng.normal(size=(T, K)).astype(np.float32), rng.normal(size=(S, K)).astype(np.float32)
+    ep = crisp.epilogue(relu=True)
+    q = lambda a: fp8.quantize(torch.from_numpy(a).cuda())
+    clean = fp8.product(q(x), q(w), out_dtype=dtype)
+    assert torch.equal(fp8.product(q(x), q(w), out_dtype=dtype, ep=ep), clean.clamp(min=0))
+    x[1, 3], x[T - 1, K - 1], w[20, 7] = np.nan, np.inf, -np.inf
+    bad = torch.zeros((T, S), dtype=torch.bool, device="cuda")
+    bad[1], bad[T - 1], bad[:, 20] = True, True, True
+    for y in (fp8.product(q(x), q(w), out_dtype=dtype, ep=ep), fp8.linear(torch.from_numpy(x).cuda(), q(w), out_dtype=dtype, ep=ep)):
+        assert y[bad].isnan().all() and torch.equal(y[~bad], clean[~bad].clamp(min=0))
+
+
 @pytest.mark.parametrize("shape", [(1, 1, 5), (1, 300, 4096), (2, 64, 256), (4, 513, 1100), (7, 96, 384), (8, 256, 8192), (1, 33, 16384), (1, 50, 16385), (2, 200, 8000), (16, 40, 1024),
                                    (15, 512, 1000), (17, 64, 128), (13, 700, 2050),
                                    (16, 128, 128), (33, 200, 1152), (300, 264, 640)], ids=str)
