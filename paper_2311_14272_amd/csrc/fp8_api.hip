@@ -79,7 +79,7 @@ crisp_status crisp_fp8_product(const crisp_fp8_mat* X, const crisp_fp8_mat* W, v
 }
 
 size_t crisp_fp8_linear_ws(int64_t T, int64_t K) {
-    if (T < 1 || K < 1 || T > MOST || K > MOST || too_many(T, K) || fp8_takes_raw(T, K)) return 0;
+    if (T < 1 || K < 1 || T > MOST || K > MOST || too_many(T, K) || fp8_takes_raw(T, blocks(K))) return 0;
     return (size_t)T * blocks(K) * (FP8_BLOCK + sizeof(float));
 }
 
@@ -98,7 +98,7 @@ crisp_status crisp_fp8_linear(const void* X, int32_t in_type, int64_t T, int64_t
     if (st != CRISP_OK || (st = check_in(X, in_type, T, W->cols, ldx)) != CRISP_OK) return st;
     if ((st = check_out(Y, T, W->rows, W->ld, ldy, y_type, ep)) != CRISP_OK) return st;
     hipError_t e;
-    if (fp8_takes_raw(T, W->cols)) {
+    if (fp8_takes_raw(T, blocks(W->cols))) {
         e = launch_fp8_raw(X, in_type, T, ldx, *W, Y, ldy, y_type, ep, (hipStream_t)stream);
     } else {
         if (off(ws, 16)) return CRISP_EALIGN;

@@ -29,9 +29,7 @@ struct ProductArgs {
     int raw_bf16, K;
 };
 
-// Blocks of X that a workgroup of fp8_split_kernel quantises for itself.  Its 512 or 1024 threads take 32 or 64 of them in
-// 0.2 us; a launch of the quantiser's own costs 2 us more on the GPU and 3 on the host.
-constexpr int FP8_OWN_BLOCKS = 128;
+inline Fp8Size size_of(const ProductArgs& a) { return Fp8Size{a.T, a.S, a.kb, a.y_bf16 != 0, a.w_tiles != 0}; }
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -110,12 +108,8 @@ __device__ __forceinline__ void store_row(const ProductArgs& a, int64_t t, int s
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st);
-// Two products in one launch: whether (not 0) and how, and the launch.  Results are those of two launches.
-int fp8_pairs(const ProductArgs& a, const ProductArgs& b);
+// Two products in one launch, as fp8_pairs says (not 0).  Results are those of two launches.
 hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b, hipStream_t st);
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st);
-// Microseconds that either kernel is expected to take.
-float fp8_tiled_time(const ProductArgs& a);
-float fp8_split_time(const ProductArgs& a);
 
 }  // namespace crisp

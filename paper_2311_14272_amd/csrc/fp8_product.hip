@@ -1,4 +1,4 @@
-// The 8-bit product's launcher: which kernel takes which sizes.
+// The 8-bit product's launchers.
 #include "fp8_product.h"
 
 namespace crisp {
@@ -19,17 +19,7 @@ static ProductArgs args_of(const crisp_fp8_mat& X, const crisp_fp8_mat& W, void*
     return a;
 }
 
-// Few rows of X or of W: no staging, the waves split the contraction - but where many rows of the other one fill the CUs with tiles (32 x 28672 x
-// 4096, us: 28 against 45; 32 x 4096 x 11008: 27 against 22; 16384 x 32 x 4096: 14 against 20).  The tiled kernel's estimate is for
-// operands in the caches; from memory bf16 results take 1.1 times as long (fp32, bound by the widening, 0.95), and no less than the reads at
-// 4.3 TB/s.  What one launch could have done
-// together with the quantiser is summed in that launch's order.  The tiled kernels' offsets inside a tile are 32 bits.
-static bool takes_split(const ProductArgs& a) {
-    if (!fp8_may_split(a.T, a.S, a.ldx > a.ldw ? a.ldx : a.ldw)) return false;
-    if (a.ldx >= 1 << 24 || a.ldw >= 1 << 24 || fp8_takes_raw(a.T, a.K)) return true;
-    const float tiled = (a.y_bf16 ? 1.1f : 0.95f) * fp8_tiled_time(a), read = 2.0f + ((float)a.T + (float)a.S) * (float)a.kb * (128e-6f / 4.3f);
-    return fp8_split_time(a) < (tiled > read ? tiled : read);
-}
+static bool takes_split(const ProductArgs& a) { return fp8_takes_split(size_of(a), a.ldx > a.ldw ? a.ldx : a.ldw); }
 
 static hipError_t launch_product(const ProductArgs& a, hipStream_t st) { return takes_split(a) ? launch_fp8_split(a, st) : launch_fp8_tiled(a, st); }
 
@@ -41,13 +31,11 @@ hipError_t launch_fp8_product(const crisp_fp8_mat& X, const crisp_fp8_mat& W, vo
 hipError_t launch_fp8_gradients(const crisp_fp8_mat& G, const crisp_fp8_mat& Wt, void* dX, int64_t lddx, int dx_type, const crisp_fp8_mat& Gt,
                                 const crisp_fp8_mat& Xt, void* dW, int64_t lddw, int dw_type, const crisp_epilogue* ep, hipStream_t st) {
     const ProductArgs a = args_of(G, Wt, dX, lddx, dx_type, nullptr), b = args_of(Gt, Xt, dW, lddw, dw_type, ep);
-    const int pairs = takes_split(a) || takes_split(b) ? 0 : fp8_pairs(a, b);
+    const int pairs = takes_split(a) || takes_split(b) ? 0 : fp8_pairs(size_of(a), size_of(b));
     if (pairs) return launch_fp8_pair(pairs, a, b, st);
     const hipError_t e = launch_product(a, st);
     return e == hipSuccess ? launch_product(b, st) : e;
 }
-
-bool fp8_takes_raw(int64_t T, int64_t K) { return T <= 16 && T * ((K + FP8_BLOCK - 1) / FP8_BLOCK) <= FP8_OWN_BLOCKS; }
 
 hipError_t launch_fp8_raw(const void* X, int in_type, int64_t T, int64_t ldx, const crisp_fp8_mat& W, void* Y, int64_t ldy, int y_type,
                           const crisp_epilogue* ep, hipStream_t st) {

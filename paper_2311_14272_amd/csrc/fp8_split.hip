@@ -163,32 +163,10 @@ static void launch_split(const ProductArgs& a, hipStream_t st) {
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * WAVES, 0, st>>>(a, ts);
 }
 
-// Two blocks requested at a time: with four, 16 x 512 x 1152 takes 6.1 us instead of 4.4 (what is requested behind the last block is
-// fetched for nothing) and 4 x 4096 x 11008 16.0 instead of 14.7.  16 waves where they get two blocks each: 1 x 4096 x 4096 6.3 us against
-// 6.9, 13 x 11008 x 4096 14.1 against 14.9.  More rows of X in a workgroup never pay: 32 x 512 x 1152 5.3 us with 32 of them, 4.4 with 16.
-static int waves_of(const ProductArgs& a) { return a.kb >= 32 ? 16 : 8; }
-
-// Microseconds with 16 ms rows of W in a workgroup, fitted to 23 sizes of 1 x 512 x 1152 to 32 x 28672 x 4096 and 64 x 8 x 4096 to 16384 x 32 x
-// 11008 whose weights come from memory: what the workgroups read (10 TB/s, mostly out of caches; as if the last round of CUs were full), their
-// number, and a wave's way through its blocks.  Two tiles of W share X's reads: 32 x 4096 x 4096 9.4 us against 11.2, 1 x 4096 x 4096 7.9
-// against 6.3.
-static float estimate(const ProductArgs& a, int ms) {
-    static const float c[2][5] = {{2.2f, 0.112f, 0.096f, 0.82f, 0.039f}, {2.9f, 0.010f, 0.120f, 0.36f, 0.071f}};
-    const float* k = c[ms - 1];
-    const int waves = waves_of(a);
-    const int64_t n = (int64_t)((a.S + 16 * ms - 1) / (16 * ms)) * ((a.T + 15) / 16);
-    const float mb = (float)a.kb * 128e-6f * (float)(min(16 * ms, a.S) + min(16, a.T)), all = k[1] * (float)n * mb, rounds = k[2] * (float)((n + 255) / 256 * 256) * mb;
-    return k[0] + (all > rounds ? all : rounds) + k[3] * (float)((a.kb + 2 * waves - 1) / (2 * waves)) + k[4] * (float)waves * (float)n / 256.0f;
-}
-
-float fp8_split_time(const ProductArgs& a) {
-    const float one = estimate(a, 1), two = estimate(a, 2);
-    return one < two ? one : two;
-}
-
 // (the sums' order depends on the number of waves alone)
 hipError_t launch_fp8_split(const ProductArgs& a, hipStream_t st) {
-    const bool many = waves_of(a) == 16, two = estimate(a, 2) < estimate(a, 1);
+    const Fp8Size z = size_of(a);
+    const bool many = fp8_split_waves(z.kb) == 16, two = fp8_split_estimate(z, 2) < fp8_split_estimate(z, 1);
     if (a.raw) many ? launch_split<1, 1, 2, 16, true>(a, st) : launch_split<1, 1, 2, 8, true>(a, st);
     else if (two) many ? launch_split<2, 1, 2, 16>(a, st) : launch_split<2, 1, 2, 8>(a, st);
     else many ? launch_split<1, 1, 2, 16>(a, st) : launch_split<1, 1, 2, 8>(a, st);

@@ -396,81 +396,6 @@ static void launch_tiles(const ProductArgs& a, hipStream_t st) {
     kernel<<<(unsigned)ts * (unsigned)tt, 64 * NS * NT * KG, 0, st>>>(a, ts, tt);
 }
 
-// The tile and its stages by estimated time.  Kernels of one workgroup a CU (their stages fill its LDS) take, for each round of 256 of
-// them, a first request and a last store that nothing hides and a time for each block.  Of those with one or two small stages
-// several run on a CU and hide these from each other: the work of a CU's tiles counts once a tile, or the way through the blocks
-// once for as many as run together.  So small tiles win where the results' way out bounds the time (few blocks) or their number
-// does not fill the last round, large ones where the matrix cores do.
-//
-// Constants in microseconds, fitted to the times of 266 sizes of 33 x 33 x 16 to 9000 x 12000 x 9000 for each type; the rule's choices take
-// 2 % longer than the best of twelve to fourteen shapes, in the geometric mean.  A few sizes, us (the rule's choices marked; --: no registers
-// for it; not built: 128 x 64 for bf16, 192 x 128 for fp32, 128 x 256):
-//
-//                          5632 x 2614 x 16   8192 x 5120 x 256    1280 x 3456 x 1840     4096 x 4096 x 4096
-//                           fp32    bf16        fp32    bf16         fp32    bf16           fp32    bf16
-//   64 x 64, two groups     51.3    41.4       135.6   112.4         47.1    32.0          236.3   158.2
-//   64 x 64, one stage      17.3*   11.6*       48.1*   28.8*        30.1    21.2          169.1   109.8
-//   64 x 64, two stages     18.6    14.2        50.4    36.6         31.5*   24.1          169.5   111.1
-//   128 x 64, two stages    19.0    14.1        51.5    36.5         30.7    20.8          157.8    91.9
-//   128 x 128, two stages   21.0    14.5        51.4    36.5         34.9    18.1          142.1*   73.9
-//   the same, 8 waves       23.0    12.8        56.1    29.2         42.7    19.7          167.9    75.2
-//   192 x 128               24.5    17.4        59.1    41.4         31.0    17.3*         163.6    87.8
-//   128 x 256, 3 stages     22.8    15.2        53.3    36.4         36.2    19.9          138.6    75.6
-//   256 x 256                 --    15.9          --    37.6           --    27.4             --    63.3*
-struct Times { float base, tile, block, way; };          // a launch; a tile's ends; a tile's block; a block's way
-struct Shape { int bs, bt, together; Times t[3]; };      // fp32; bf16: W tiles, W rows; 0: not built
-constexpr int SHAPES = 10;
-static const Shape shapes[SHAPES] = {
-    {64, 64, 1, {{1.75f, 2.88f, 0.37f, 0}, {1.76f, 2.45f, 0.215f, 0}, {1.6f, 2.3f, 0.23f, 0}}},               // two groups
-    {64, 64, 5, {{3.33f, 0.56f, 0.32f, 0.74f}, {3.4f, 0.24f, 0.20f, 0.49f}, {3.0f, 0.25f, 0.22f, 0.65f}}},    // one stage
-    {64, 64, 4, {{3.54f, 0.66f, 0.31f, 0.49f}, {2.9f, 0.54f, 0.19f, 0.37f}, {2.93f, 0.47f, 0.205f, 0.38f}}},  // two stages
-    {128, 64, 1, {{}, {1.62f, 3.67f, 0.31f, 0}, {1.44f, 3.78f, 0.35f, 0}}},                                   // two groups
-    {128, 64, 3, {{3.52f, 1.43f, 0.54f, 0.73f}, {}, {}}},                                                     // two stages
-    {128, 128, 1, {{}, {1.21f, 3.90f, 0.48f, 0}, {}}},                                                        // four stages
-    {128, 128, 2, {{3.56f, 3.09f, 0.92f, 1.09f}, {3.12f, 1.77f, 0.49f, 0.52f}, {2.8f, 1.76f, 0.57f, 0.64f}}}, // two stages; bf16: 8 waves
-    {192, 128, 1, {{}, {0.39f, 5.09f, 0.72f, 0}, {0.32f, 5.9f, 0.86f, 0}}},
-    {192, 256, 1, {{}, {0.0f, 8.2f, 1.04f, 0}, {0.0f, 8.3f, 1.3f, 0}}},
-    {256, 256, 1, {{}, {0.0f, 12.0f, 1.25f, 0}, {}}}};
-
-static int type_of(const ProductArgs& a) { return !a.y_bf16 ? 0 : a.w_tiles ? 1 : 2; }
-static int64_t tiles_of(const Shape& s, const ProductArgs& a) { return (int64_t)((a.S + s.bs - 1) / s.bs) * ((a.T + s.bt - 1) / s.bt); }
-
-static float estimate(const Shape& s, const Times& t, int64_t tiles, int kb) {
-    const int64_t m = (tiles + 255) / 256;
-    const float work = (float)m * t.block, way = (float)((m + s.together - 1) / s.together) * t.way;
-    return t.base + (float)m * t.tile + (float)kb * (work > way ? work : way);
-}
-
-static float estimate(int shape, const ProductArgs& a) { return estimate(shapes[shape], shapes[shape].t[type_of(a)], tiles_of(shapes[shape], a), a.kb); }
-
-// Two groups add their sums in an order of their own; the other shapes have the same bits.
-static bool grouped(int shape) { return shape == 0 || shape == 3; }
-
-// Two groups from twelve blocks on: at nine they gain 0.2 to 0.5 us (512 x 512 x 1152: 6.1 against 6.3, fp32 7.5 against 8.0), and a layer's two
-// gradients, one of them of few blocks, then rarely have a launch in common (256 x 1024 x 1024 with the quantiser: 14.9 us apart, 12.3 together).
-static int tile_shape(const ProductArgs& a) {
-    int best = -1;
-    for (int k = 0; k < SHAPES; ++k) {
-        if (shapes[k].t[type_of(a)].block == 0.0f || (grouped(k) && a.kb < 12)) continue;
-        if (best < 0 || estimate(k, a) < estimate(best, a)) best = k;
-    }
-    return best;
-}
-
-float fp8_tiled_time(const ProductArgs& a) { return estimate(tile_shape(a), a); }
-
-// Two products in one launch of 64 x 64 tiles, of two groups or of two stages: where neither result changes by it and that takes less time
-// than two launches.  0: not.
-int fp8_pairs(const ProductArgs& a, const ProductArgs& b) {
-    if (!a.y_bf16 || !a.w_tiles || b.y_bf16 || b.w_tiles) return 0;
-    const int sa = tile_shape(a), sb = tile_shape(b);
-    if (grouped(sa) != grouped(sb)) return 0;
-    const int k = grouped(sa) ? 0 : 2;
-    const int64_t tiles = tiles_of(shapes[k], a) + tiles_of(shapes[k], b);
-    const float ea = estimate(shapes[k], shapes[k].t[1], tiles, a.kb), eb = estimate(shapes[k], shapes[k].t[0], tiles, b.kb);
-    return (ea > eb ? ea : eb) < estimate(sa, a) + estimate(sb, b) ? 2 - grouped(sa) : 0;
-}
-
 hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b, hipStream_t st) {
     const int as = (a.S + 63) / 64, at = (a.T + 63) / 64, bs = (b.S + 63) / 64, bt = (b.T + 63) / 64;
     const unsigned grid = (unsigned)(as * at + bs * bt);
@@ -480,7 +405,7 @@ hipError_t launch_fp8_pair(int pairs, const ProductArgs& a, const ProductArgs& b
 }
 
 hipError_t launch_fp8_tiled(const ProductArgs& a, hipStream_t st) {
-    switch (tile_shape(a) * 2 + a.y_bf16) {
+    switch (fp8_tile_shape(size_of(a)) * 2 + a.y_bf16) {
         case 0: launch_tiles<2, 2, 1, 1, 3, 2, false>(a, st); break;
         case 1: launch_tiles<2, 2, 1, 1, 3, 2, true>(a, st); break;
         case 2: launch_tiles<2, 2, 1, 1, 1, 1, false>(a, st); break;
