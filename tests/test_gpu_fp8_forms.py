@@ -146,3 +146,25 @@ def test_what_the_8_bit_instruction_cuts(shape):
     check(U.product_bound)
     x[:, ::8], w[:, ::8] = 256.0, 256.0 * alternate
     check(U.product_bound_fast)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(5, 48, 512), (300, 264, 640), (3085, 2651, 256)], ids=str)
+def test_scales_that_multiply_to_a_subnormal(shape, dtype):
+    """Scales of 2^-64 to 2^-80 each: their products lie between 2^-128 and 2^-160, and are off by up to half of 2^-149; the results are what
+    those leave.  Blocks of zeros, whose scale is 2^-126, stay zeros."""
+    T, S, K = shape
+    g = torch.Generator(device="cuda").manual_seed(T)
+    X, W = (_exact(g, rows, K, False)[0] for rows in (T, S))
+    for m in (X, W):
+        m.scale.copy_(torch.exp2(-64 - 16 * torch.rand(m.scale.shape, generator=g, device="cuda")))
+        m.scale[0], m.q[:, :128] = 2.0 ** -126, torch.zeros((), dtype=torch.float8_e4m3fn, device="cuda")
+    k = -(-K // 128) * 128
+    q, s = [m.q[:, :k].double() for m in (X, W)], [m.scale.t().double().repeat_interleave(128, 1) for m in (X, W)]
+    held = [a * b for a, b in zip(q, s)]
+    want, size = held[0] @ held[1].t().contiguous(), held[0].abs() @ held[1].abs().t().contiguous()
+    # a block's sum times the half step of its factor, and half a step of each of the block's additions and of the result; the sums are exact
+    slack = 2.0 ** -150 * (q[0].abs() @ q[1].abs().t().contiguous()) + 2.0 ** -150 * (K // 128 + 2) + (K // 128 + 3) * 2.0 ** -24 * size
+    y = fp8.product(X, W, out_dtype=dtype).double()
+    near = 2.0 ** -8 * (want.abs() + slack) + 2.0 ** -134 if dtype == torch.bfloat16 else 0.0
+    assert ((y - want).abs() <= slack + near).all() and want.abs().max() > 2.0 ** -135
