@@ -15,7 +15,8 @@ struct Fp8Size { int T, S, kb; bool bf16, w_tiles; };
 //
 // Constants in microseconds, fitted to the times of 266 sizes of 33 x 33 x 16 to 9000 x 12000 x 9000 for each type; the rule's choices take
 // 2 % longer than the best of twelve to fourteen shapes, in the geometric mean.  A few sizes, us (the rule's choices marked; --: no registers
-// for it; not built: 128 x 64 for bf16, 192 x 128 for fp32, 128 x 256):
+// for it; not built: 128 x 64 for bf16, 192 x 128 for fp32, 128 x 256, which gains 2.5 % at the last size for fp32 and is behind
+// at the others):
 //
 //                          5632 x 2614 x 16   8192 x 5120 x 256    1280 x 3456 x 1840     4096 x 4096 x 4096
 //                           fp32    bf16        fp32    bf16         fp32    bf16           fp32    bf16
@@ -85,7 +86,7 @@ inline int fp8_pairs(const Fp8Size& a, const Fp8Size& b) {
 
 // Two blocks requested at a time: with four, 16 x 512 x 1152 takes 6.1 us instead of 4.4 (what is requested behind the last block is
 // fetched for nothing) and 4 x 4096 x 11008 16.0 instead of 14.7.  16 waves where they get two blocks each: 1 x 4096 x 4096 6.3 us against
-// 6.9, 13 x 11008 x 4096 14.1 against 14.9.  More rows of X in a workgroup never pay: 32 x 512 x 1152 5.3 us with 32 of them, 4.4 with 16.
+// 6.9, 2 x 11008 x 4096 12.0 against 12.7.  More rows of X in a workgroup never pay: 32 x 512 x 1152 5.3 us with 32 of them, 4.4 with 16.
 inline int fp8_split_waves(int kb) { return kb >= 32 ? 16 : 8; }
 
 // Microseconds with 16 ms rows of W in a workgroup, fitted to 23 sizes of 1 x 512 x 1152 to 32 x 28672 x 4096 and 64 x 8 x 4096 to 16384 x 32 x
