@@ -31,7 +31,7 @@ typedef struct {
     uint16_t *w_copy;        /* optional, w_type F32 only: the new weights rounded to bf16                             */
     const uint32_t *mask;    /* optional: numel/row_len rows of ceil(row_len/32) words, bit k%32 of word k/32 set for  */
                              /* the kept columns of a row (as crisp_hybrid_mask writes it, or an nm_mask); 4-byte aligned */
-    int64_t numel;           /* >= 0; 0: nothing to do, no pointer is looked at                                        */
+    int64_t numel;           /* 0 .. 2^35; 0: nothing to do, no pointer is looked at                                   */
     int64_t row_len;         /* mask given: columns of a row, numel a multiple of it, both below 2^31; else ignored    */
     int32_t w_type, g_type;  /* CRISP_P_*                                                                              */
     int32_t moments;         /* CRISP_MOMENTS_*                                                                        */

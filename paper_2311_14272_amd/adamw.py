@@ -7,6 +7,9 @@ marshalling only, every step runs in the HIP kernels.
 
 Moments are fp32 tensors, or e4m3 ones (torch.float8_e4m3fn or uint8) with a scale for each 128 elements (m_scale, v_scale);
 alloc_moments makes either.  Tensors live on the current device; work goes to the current stream.
+
+Autograd does not see a step: weights change in place and keep their version, so a graph that was recorded before the step must
+not be run backward after it.
 """
 from __future__ import annotations
 

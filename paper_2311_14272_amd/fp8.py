@@ -10,6 +10,9 @@ gradients) or of 128 x 128 elements (TILES, weights).  One layer's training step
     dx, dw = linear_backward(dy, x_t, w_t)       # T x K and S x K, dw in fp32: the gradient crisp_select_mask and adamw take
 
 and serving is y = linear(x, w8).  Tensors live on the current device; work goes to the current stream.
+
+Autograd does not see these calls: a result carries no gradient, also where an argument requires one, and linear_backward is
+called by hand.  A bias's gradient, the sum of dy's rows, is not among its results.
 """
 from __future__ import annotations
 
