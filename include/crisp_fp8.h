@@ -9,7 +9,7 @@
  *
  * The conventions of crisp.h hold: status codes, arguments checked on the host before any device call, no allocation and
  * no synchronisation, work enqueued on `stream`.  What a call writes must not overlap what it reads, but for a residual that is
- * Y itself.
+ * Y itself, nor its other results (EINVAL where two of them begin at the same address).
  */
 #ifndef CRISP_FP8_H
 #define CRISP_FP8_H

@@ -64,6 +64,7 @@ crisp_status crisp_fp8_quant(const void* X, int32_t in_type, int64_t rows, int64
     if (Q && Qt && Q->kind != Qt->kind) return CRISP_EINVAL;
     if ((Q && (Q->rows != rows || Q->cols != cols)) || (Qt && (Qt->rows != cols || Qt->cols != rows))) return CRISP_ESHAPE;
     if (off(mask, 4)) return CRISP_EALIGN;
+    if (Q && Qt && (Q->q == Qt->q || Q->scale == Qt->scale)) return CRISP_EINVAL;
     return launch_fp8_quant(X, in_type, rows, cols, ldx, mask, Q, Qt, (hipStream_t)stream) == hipSuccess ? CRISP_OK : CRISP_EDEVICE;
 }
 
@@ -138,6 +139,7 @@ crisp_status crisp_fp8_linear_backward(const void* dY, int32_t in_type, int64_t 
     }
     if (off(ws, 16)) return CRISP_EALIGN;
     if (!ws || ws_bytes < crisp_fp8_linear_backward_ws(T, S)) return CRISP_EBUFSIZE;
+    if (dX == dW) return CRISP_EINVAL;
     const crisp_fp8_mat g = mat_in(ws, T, S), gt = mat_in(static_cast<uint8_t*>(ws) + mat_bytes(T, S), S, T);
     hipError_t e = launch_fp8_quant(dY, in_type, T, S, ldg, nullptr, dX ? &g : nullptr, dW ? &gt : nullptr, (hipStream_t)stream);
     if (e == hipSuccess && dX && dW) e = launch_fp8_gradients(g, *Wt, dX, lddx, dx_type, gt, *Xt, dW, lddw, dw_type, ep, (hipStream_t)stream);

@@ -75,6 +75,16 @@ def test_quant_refusals():
     assert _quant(rows=1 << 27, cols=512, Q=_mat(1 << 27, 512)) == crisp.ESHAPE     # 2^29 blocks of a row
 
 
+def test_two_results_in_one_place_are_refused():
+    """A square matrix and its transpose, or a layer's two gradients, cannot go to the same buffer: which of the two stayed would be chance."""
+    at = lambda q, scale: _mat(256, 256, q=FAKE * q, scale=FAKE * scale)
+    for Qt in (at(1, 7), at(7, 1), at(1, 1)):
+        assert _quant(rows=256, cols=256, Q=at(1, 1), Qt=Qt) == crisp.EINVAL
+    L = fp8.lib()
+    m, need = _mat(256, 256), L.crisp_fp8_linear_backward_ws(256, 256)
+    assert L.crisp_fp8_linear_backward(FAKE, 1, 256, 256, 256, C.byref(m), C.byref(m), 64 * FAKE, 256, 0, 64 * FAKE, 256, 0, 0, FAKE, need, None) == crisp.EINVAL
+
+
 def _product(X=None, W=None, Y=FAKE, ldy=64, t=1, ep=None):
     X, W = X or _mat(16, 256), W or _mat(64, 256, fp8.TILES)
     return fp8.lib().crisp_fp8_product(C.byref(X), C.byref(W), Y, ldy, t, C.byref(ep) if ep else None, None)
